@@ -27,7 +27,8 @@ enum {
     ATTN_E_UNSUPPORTED = -3,  /* D != 128, or a tensor too large for the kernel's index math   */
     ATTN_E_ALIGN       = -4,  /* q, k, v or o not 16-byte aligned, or lse not 4-byte aligned   */
     ATTN_E_SCALE       = -5,  /* scale is NaN or infinite                                      */
-    ATTN_E_LAUNCH      = -6   /* the HIP runtime refused the launch                            */
+    ATTN_E_LAUNCH      = -6,  /* the HIP runtime refused the launch                            */
+    ATTN_E_WORKSPACE   = -7   /* a workspace is smaller than needed (attn_layer.h)             */
 };
 
 /*

@@ -1,7 +1,8 @@
-"""MI355X-native fused attention forward: thin Python binding over the C ABI of include/attn.h.
+"""MI355X-native fused attention, and what stands around it in a layer: thin Python binding over the C ABIs of include/attn.h
+(the forward pass) and include/attn_layer.h (its backward pass; norm and rotation of queries and keys, and their gradient).
 
 Argument marshalling only (attention() does it natively, in csrc/attn_call.cpp): every step of the
-computation runs in the HIP kernels of csrc/attn_fwd.hip.  There is no CPU or PyTorch fallback; if the
+computation runs in the HIP kernels of csrc/*.hip.  The differentiable forms are in autograd.py.  There is no CPU or PyTorch fallback; if the
 shared library has not been built, importing the entry points fails loudly.
 """
 import ctypes
@@ -18,14 +19,15 @@ ATTN_E_UNSUPPORTED = -3
 ATTN_E_ALIGN = -4
 ATTN_E_SCALE = -5
 ATTN_E_LAUNCH = -6
+ATTN_E_WORKSPACE = -7
 
 _lib = None
 
 
 class AttnError(RuntimeError):
-    def __init__(self, code):
+    def __init__(self, code, what="attn_fwd"):
         self.code = code
-        super().__init__(f"attn_fwd failed ({code}): {attn_strerror(code)}")
+        super().__init__(f"{what} failed ({code}): {attn_strerror(code)}")
 
 
 def open_library(path):
@@ -149,3 +151,7 @@ def _attention(q, k, v, causal, scale):
     if rc != ATTN_OK:
         raise AttnError(rc)
     return o, lse
+
+
+from .layer import (attention_backward, attn_bwd, attn_bwd_workspace, load_layer, qk_norm_rope,  # noqa: E402,F401
+                    qk_norm_rope_backward, rope_table)

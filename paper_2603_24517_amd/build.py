@@ -1,6 +1,7 @@
 """Build the gfx950 shared libraries in-tree with hipcc.
 
-    python -m paper_2603_24517_amd.build            the attention library (C ABI of include/attn.h) and the binding's native part
+    python -m paper_2603_24517_amd.build            the attention library (C ABI of include/attn.h), the library of the operators
+                                                     around it (include/attn_layer.h) and the binding's native part
     python -m paper_2603_24517_amd.build --all      that, the measurement-aid library (include/attn_probe.h)
                                                      and every variant of the attention kernel
 
@@ -18,6 +19,8 @@ LIB = os.path.join(HERE, "libattn_mi355x.so")
 PROBE_SRC = os.path.join(HERE, "csrc", "attn_probe.hip")
 PROBE_LIB = os.path.join(HERE, "libattn_probe.so")
 VARIANT_DIR = os.path.join(HERE, "variants")
+LAYER_SRCS = [os.path.join(HERE, "csrc", n) for n in ("attn_bwd.hip", "qk_norm_rope.hip")]
+LAYER_LIB = os.path.join(HERE, "libattn_layer_mi355x.so")
 CALL_SRC = os.path.join(HERE, "csrc", "attn_call.cpp")
 CALL_LIB = os.path.join(HERE, "_attn_call.so")
 
@@ -26,6 +29,10 @@ HIPCC_FLAGS = [
     # packed FP32 VALU forms are kept out of the generated code on purpose
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
+
+# Matrix products may accumulate in either half of the register file, chosen for each product, not for a whole kernel: the backward kernel
+# keeps its sums in one half and its scores, which vector instructions read, in the other.  (Without it 268 registers of that kernel spill.)
+LAYER_FLAGS = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 
 # every launch through the 256-row kernel, in whole items: for switches that act there
 ALL_256_ROWS = ["-DATTN_SMALL_PATH=0", "-DATTN_SHARE=0"]
@@ -63,7 +70,7 @@ def variant_path(name):
 
 def _hipcc(flags, out, src, verbose):
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *HIPCC_FLAGS, *flags, "-o", out, src]
+    cmd = [hipcc, *HIPCC_FLAGS, *flags, "-o", out, *([src] if isinstance(src, str) else src)]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
@@ -76,6 +83,10 @@ def build_library(extra_flags=(), out=LIB, verbose=False):
 
 def build_probe(verbose=False):
     return _hipcc([], PROBE_LIB, PROBE_SRC, verbose)
+
+
+def build_layer(verbose=False):
+    return _hipcc(LAYER_FLAGS, LAYER_LIB, LAYER_SRCS, verbose)
 
 
 def build_call(verbose=False):
@@ -102,7 +113,7 @@ def build_all(verbose=False, jobs=4):
     """Everything, a few compilations at a time (each is a single-threaded hipcc run of about ten seconds)."""
     from concurrent.futures import ThreadPoolExecutor
     os.makedirs(VARIANT_DIR, exist_ok=True)
-    tasks = [lambda: build_call(verbose=verbose), lambda: build_library(verbose=verbose), lambda: build_probe(verbose=verbose)]
+    tasks = [lambda: build_call(verbose=verbose), lambda: build_layer(verbose=verbose), lambda: build_library(verbose=verbose), lambda: build_probe(verbose=verbose)]
     tasks += [lambda n=n: build_library(VARIANTS[n], variant_path(n), verbose) for n in VARIANTS]
     with ThreadPoolExecutor(max_workers=jobs) as pool:
         for f in [pool.submit(t) for t in tasks]:
@@ -114,4 +125,5 @@ if __name__ == "__main__":
         build_all(verbose=True)
     else:
         print(build_library(extra_flags=sys.argv[1:], verbose=True))
+        print(build_layer(verbose=True))
         print(build_call(verbose=True))

@@ -11,16 +11,29 @@ FIELDS = ("vgpr_count", "agpr_count", "sgpr_count", "vgpr_spill_count", "sgpr_sp
           "private_segment_fixed_size", "group_segment_fixed_size", "max_flat_workgroup_size")
 
 
+def _bundles(fatbin):
+    """The bundles of a library's section: one for each translation unit with device code."""
+    magic = b"__CLANG_OFFLOAD_BUNDLE__"
+    starts = [m.start() for m in re.finditer(magic, fatbin)]
+    return [fatbin[a:b] for a, b in zip(starts, starts[1:] + [len(fatbin)])]
+
+
 def kernel_metadata(lib_path):
-    """{kernel symbol: {field: int}} for every kernel of the library's gfx950 code object."""
+    """{kernel symbol: {field: int}} for every kernel of the library's gfx950 code objects."""
+    notes = ""
     with tempfile.TemporaryDirectory() as tmp:
-        fatbin, code = os.path.join(tmp, "fatbin"), os.path.join(tmp, "code.o")
+        fatbin, part, code = (os.path.join(tmp, n) for n in ("fatbin", "part", "code.o"))
         subprocess.run([os.path.join(LLVM_BIN, "llvm-objcopy"), "-O", "binary", "--only-section=.hip_fatbin",
                         lib_path, fatbin], check=True)
-        subprocess.run([os.path.join(LLVM_BIN, "clang-offload-bundler"), "--unbundle", "--type=o",
-                        f"--targets={TARGET}", f"--input={fatbin}", f"--output={code}"], check=True)
-        notes = subprocess.run([os.path.join(LLVM_BIN, "llvm-readelf"), "--notes", code], check=True,
-                               capture_output=True, text=True).stdout
+        with open(fatbin, "rb") as f:
+            bundles = _bundles(f.read())
+        for bundle in bundles:
+            with open(part, "wb") as f:
+                f.write(bundle)
+            subprocess.run([os.path.join(LLVM_BIN, "clang-offload-bundler"), "--unbundle", "--type=o",
+                            f"--targets={TARGET}", f"--input={part}", f"--output={code}"], check=True)
+            notes += subprocess.run([os.path.join(LLVM_BIN, "llvm-readelf"), "--notes", code], check=True,
+                                    capture_output=True, text=True).stdout
     kernels = {}
     for entry in re.split(r"\n\s*- \.", notes):
         name = re.search(r"\.name:\s+(\S+)", entry)

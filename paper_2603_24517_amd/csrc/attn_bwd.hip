@@ -1,0 +1,626 @@
+// Attention backward for MI355X (gfx950, CDNA4): dQ, dK and dV from dO, O and LSE, the probabilities recomputed tile by tile.
+//
+// With P = exp(scale * Q K^T - LSE) and dS = P * (dO V^T - delta), delta = rowsum(dO * O) - dLSE:
+//     dV = P^T dO        dK = scale * dS^T Q        dQ = scale * dS K
+//
+// Three launches: delta and LSE in the units and the layout that the kernel wants (attn_bwd_stats); the products
+// (attn_bwd_kernel); and, where items were cut into parts, the sum of the parts (attn_bwd_join).
+//
+// dK and dV are sums over queries, dQ is one over keys.  One pass for all three would have to add up dQ in memory across
+// workgroups (atomics: another order, other bits, every launch, and 16 KiB of FP32 through the caches for 32 rows).
+// Here a work item holds one side in registers and streams the other, and the scores are formed in both kinds of items: seven products
+// instead of five, but no memory traffic beside inputs and outputs, and the same bits always.
+//   * a "keys" item holds K and V of 128 * NT keys and streams Q and dO of every query head that shares them;
+//   * a "rows" item holds Q and dO of 128 * NT query rows and streams K and V.
+// Both are the same loop with the operands' names exchanged.  X1, X2 stand for what is held, Y1, Y2 for what streams:
+//     S = Y1 X1^T     dP = Y2 X2^T - delta     acc1 += Y1^T dS     (keys only) acc2 += Y2^T P
+// With v_mfma_f32_32x32x16_bf16 and Y as the A operand, the accumulator layout puts one held row (lane % 32) in each lane
+// and 16 of the tile's 32 streamed rows in its registers, so P and dS are, packed to BF16 in registers, directly the B operands of the
+// products with Y^T, which the transposing read ds_read_b64_tr_b16 fetches from the same tile in LDS: nothing
+// of size rows x keys leaves the registers.
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+#include <math.h>
+#include <atomic>
+#include <type_traits>
+
+#include "../../include/attn.h"
+#include "../../include/attn_layer.h"
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+#define LDS_AS __attribute__((address_space(3)))
+
+constexpr int HD = 128;
+constexpr int ROW_BYTES = HD * 2;
+constexpr int BT = 32;                          // streamed rows per step
+constexpr int TILE_BYTES = BT * ROW_BYTES;      // 8 KiB
+constexpr int NSTAGE = 3;
+constexpr int STATS_BYTES = 2 * BT * 4;         // -LSE and -delta of a step's 32 rows
+constexpr int STAGE_BYTES = 2 * TILE_BYTES + 4 * STATS_BYTES;   // (each wavefront has the figures for itself)
+constexpr int X2_BASE = NSTAGE * STAGE_BYTES;   // keys items with NT = 2: V, 16 KiB per wavefront
+constexpr float LOG2E = 1.4426950408889634f;
+
+constexpr int lds_bytes(int nt) { return X2_BASE + (nt == 2 ? 4 * 64 * ROW_BYTES : 0); }
+
+struct Role {
+    int groups, tiles, splits;      // items: groups x tiles x splits
+    int first;                      // number of its first item
+};
+struct Params {
+    const __bf16 *q, *k, *v, *dout;
+    __bf16 *dq, *dk, *dv;
+    const float *stats;
+    float *part_q, *part_kv;        // parts: [split][rows of dq] / [split][dk or dv][rows]
+    int B, Hq, Hkv, Sq, Skv, G, qtiles;
+    int pack, chunks;               // rows items: query heads of a group side by side, and how many such chunks a group has
+    int off;                        // key j valid for row i iff j <= i + off (without the mask: always true)
+    float c, scale;                 // c = scale * log2(e)
+    Role keys, rows;
+};
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    bf16x2 p = __builtin_convertvector((f32x2){a, b}, bf16x2);   // v_cvt_pk_bf16_f32, nearest even
+    return __builtin_bit_cast(uint32_t, p);
+}
+__device__ __forceinline__ const unsigned char *uniform_ptr(const unsigned char *ptr) {
+    const uint64_t v = (uint64_t)(uintptr_t)ptr;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (const unsigned char *)(uintptr_t)(((uint64_t)hi << 32) | lo);
+}
+// 16 (4) bytes per lane from global memory straight into LDS, at lds_base + 16 (4) * lane.  Inline assembly, so that the compiler's
+// count of outstanding loads does not make every LDS read wait for it; the caller waits with s_waitcnt vmcnt(n).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void lds_dma16(const unsigned char *base, uint32_t voffset, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :
+                 : "s"(lds_base), "v"(voffset), "s"(base)
+                 : "memory", "m0");
+}
+__device__ __forceinline__ void lds_dma4(const unsigned char *base, uint32_t voffset, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                 :
+                 : "s"(lds_base), "v"(voffset), "s"(base)
+                 : "memory", "m0");
+}
+#pragma clang diagnostic pop
+constexpr int wait_vmcnt(int n) { return 0x0F70 | n; }     // s_waitcnt vmcnt(n), n < 16
+__device__ __forceinline__ void wg_barrier() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// One physical 16-byte unit of a tile row: unit u of row r stands at u ^ f(r), f(r) = (r & 3) << 2 | (r >> 2) & 3.  f runs through
+// all 16 values, so 16 lanes that read one unit of 16 rows touch every bank once; and its upper bits differ within 4 rows in line, so
+// the 4 rows x 64 bytes that a half-wave fetches with the transposing read do so too: one copy of a tile serves both.
+__device__ __forceinline__ int swz(int row) { return ((row & 3) << 2) | ((row >> 2) & 3); }
+
+// ------------------------------------------------------------------------------------------------ -LSE and -delta
+// stats[(b * Hq + h) * qtiles + tile][64]: -LSE * log2(e) of the tile's 32 rows, then -delta.  Rows past the end, and rows
+// without a valid key (LSE = -inf), get -inf and 0, so that their P and dS are 0.
+__global__ __launch_bounds__(256) void attn_bwd_stats(const __bf16 *dout, const __bf16 *o, const float *lse, const float *dlse,
+                                                      float *stats, int Hq, int Sq, int qtiles, unsigned rows)
+{
+    // 16 lanes per (position, head) row, heads fastest: a wavefront reads 1 KiB in line.  Four rows each, loads first.
+    const unsigned b = blockIdx.y;
+    const int part = threadIdx.x & 15;
+    const size_t base = (size_t)b * Sq * Hq;
+    unsigned n[4];
+    bf16x8 x[4], y[4];
+    bool real[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        n[k] = blockIdx.x * 64 + k * 16 + (threadIdx.x >> 4);
+        real[k] = n[k] < (unsigned)Sq * (unsigned)Hq;
+        const size_t at = (base + (real[k] ? n[k] : 0)) * HD + part * 8;
+        x[k] = *(const bf16x8 *)(dout + at);
+        y[k] = *(const bf16x8 *)(o + at);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (n[k] >= rows) continue;
+        float s = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf((float)x[k][e], (float)y[k][e], s);
+        s += __shfl_xor(s, 1);
+        s += __shfl_xor(s, 2);
+        s += __shfl_xor(s, 4);
+        s += __shfl_xor(s, 8);
+        const unsigned i = n[k] / (unsigned)Hq, h = n[k] - i * Hq;
+        if (part == 0) {
+            float nl = -INFINITY, nd = 0.0f;
+            if (real[k]) {
+                const size_t at = ((size_t)b * Hq + h) * Sq + i;
+                const float l = lse[at];
+                if (l != -INFINITY) {
+                    nl = -l * LOG2E;
+                    nd = (dlse ? dlse[at] : 0.0f) - s;
+                }
+            }
+            float *out = stats + (((size_t)b * Hq + h) * qtiles + (i >> 5)) * (2 * BT) + (i & 31);
+            out[0] = nl;
+            out[BT] = nd;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------ the products
+// One item: KEYS holds K (X1), V (X2) and streams Q (Y1), dO (Y2); otherwise the reverse.  NT: held 32-row tiles per wavefront.
+template <bool KEYS, int NT>
+__device__ __forceinline__ void item(const Params &p, int group, int tile, int split)
+{
+    constexpr bool X2_LDS = KEYS && NT == 2;    // K, V, dK and dV of 64 keys in registers would be 384, and the scores do not fit beside them
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    LDS_AS unsigned char *lds = (LDS_AS unsigned char *)smem;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    // ---- what this wavefront holds, and the steps that it streams
+    int b, x_head, x0, x_rows, y_rows, y_head0, steps, step0;
+    if (KEYS) {
+        b = group / p.Hkv;
+        x_head = group - b * p.Hkv;
+        x0 = tile * (128 * NT) + wave * 32 * NT;
+        x_rows = p.Skv;
+        y_rows = p.Sq;
+        y_head0 = x_head * p.G;
+    } else {
+        const int bh = group / p.chunks;
+        b = bh / p.Hkv;
+        y_head0 = bh - b * p.Hkv;
+        x_head = y_head0 * p.G + (group - bh * p.chunks) * p.pack + (wave & (p.pack - 1));
+        x0 = tile * (128 * NT / p.pack) + (wave / p.pack) * 32 * NT;
+        x_rows = p.Sq;
+        y_rows = p.Skv;
+    }
+    // KEYS: query tiles t0 .. qtiles - 1 of each head; else: key tiles 0 .. t1 - 1
+    int t0 = 0, per_head;
+    if (KEYS) {
+        const int first = tile * (128 * NT) - p.off;        // first row that sees the item's first key
+        t0 = first > 0 ? min(first / BT, p.qtiles) : 0;
+        per_head = p.qtiles - t0;
+        steps = per_head * p.G;
+    } else {
+        const int last = min((tile + 1) * (128 * NT / p.pack), p.Sq) - 1 + p.off;      // last key that the item's last row sees
+        steps = last < 0 ? 0 : min(last / BT, (p.Skv - 1) / BT) + 1;
+        per_head = steps;
+    }
+    {
+        const int splits = KEYS ? p.keys.splits : p.rows.splits;
+        step0 = (int)((long long)steps * split / splits);
+        steps = (int)((long long)steps * (split + 1) / splits) - step0;
+    }
+    const int x_heads = KEYS ? p.Hkv : p.Hq, y_heads = KEYS ? p.Hq : p.Hkv;
+    const uint32_t y_stride = (uint32_t)y_heads * ROW_BYTES;
+    const unsigned char *y1 = (const unsigned char *)(KEYS ? p.q : p.k), *y2 = (const unsigned char *)(KEYS ? p.dout : p.v);
+
+    // ---- requests: 4 rows x 256 bytes per instruction, two of each tile per wavefront
+    const int ld_r = lane >> 4, ld_u = lane & 15;
+    // where requests and steps stand: streamed tile, query head of the group, LDS stage
+    struct At { int tile, head, stage; };
+    const int y_tiles = KEYS ? p.qtiles : INT32_MAX;
+    At req, cur;
+    req.head = KEYS && per_head > 0 ? step0 / per_head : 0;
+    req.tile = KEYS ? step0 - req.head * per_head + t0 : step0;
+    req.stage = 0;
+    cur = req;
+    auto next = [&](At &a) __attribute__((always_inline)) {
+        if (++a.tile == y_tiles) {
+            a.tile = t0;
+            ++a.head;
+        }
+        a.stage = a.stage == (NSTAGE - 1) * STAGE_BYTES ? 0 : a.stage + STAGE_BYTES;
+    };
+    // past the end the last step's tiles are read again, into stages that nobody reads, so that the number in flight stays the same
+    int left = steps;
+    auto request = [&]() __attribute__((always_inline)) {
+        const int s = req.tile, head = req.head;
+        const int stage = req.stage;
+        const size_t at = ((size_t)((size_t)b * y_rows + (size_t)s * BT) * y_heads + y_head0 + head) * ROW_BYTES;
+        const unsigned char *g1 = uniform_ptr(y1 + at), *g2 = uniform_ptr(y2 + at);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + stage + wave * 2048);
+        const int last = y_rows - 1 - s * BT;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = (wave * 2 + i) * 4 + ld_r;
+            const uint32_t o = (uint32_t)min(row, last) * y_stride + ((ld_u ^ swz(row)) << 4);
+            lds_dma16(g1, o, to + i * 1024);
+            lds_dma16(g2, o, to + TILE_BYTES + i * 1024);
+        }
+        if (KEYS) {
+            const float *st = p.stats + ((size_t)((size_t)b * p.Hq + y_head0 + head) * p.qtiles + s) * (2 * BT);
+            lds_dma4(uniform_ptr((const unsigned char *)st), lane * 4,
+                     __builtin_amdgcn_readfirstlane(lds0 + stage + 2 * TILE_BYTES + wave * STATS_BYTES));
+        }
+        const int tile = req.tile, h = req.head;
+        next(req);
+        if (--left <= 0) {
+            req.tile = tile;
+            req.head = h;
+        }
+    };
+    constexpr int PER_STEP = KEYS ? 5 : 4;
+
+    // ---- held operands
+    bf16x8 x1[NT][8], x2[NT][8];
+    f32x16 nd[NT];              // rows items: -delta of the lane's row in every element, the C operand that dP starts from
+    float nl[NT];
+    const LDS_AS unsigned char *x2l = lds + X2_BASE + wave * (64 * ROW_BYTES);
+    {
+        const __bf16 *g1 = KEYS ? p.k : p.q, *g2 = KEYS ? p.v : p.dout;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int row = min(x0 + 32 * t + l32, x_rows - 1);
+            const size_t at = ((size_t)((size_t)b * x_rows + row) * x_heads + x_head) * HD + 8 * hh;
+#pragma unroll
+            for (int s = 0; s < 8; ++s) x1[t][s] = *(const bf16x8 *)(g1 + at + 16 * s);
+            if (!X2_LDS) {
+#pragma unroll
+                for (int s = 0; s < 8; ++s) x2[t][s] = *(const bf16x8 *)(g2 + at + 16 * s);
+            }
+            if (!KEYS) {
+                const int i = min(x0 + 32 * t + l32, p.Sq - 1);
+                const float *st = p.stats + ((size_t)((size_t)b * p.Hq + x_head) * p.qtiles + (i >> 5)) * (2 * BT) + (i & 31);
+                nl[t] = st[0];
+                const float d = st[BT];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) nd[t][r] = d;
+            }
+        }
+        if (X2_LDS) {
+            const int first = min(x0, x_rows - 1), last = x_rows - 1 - first;
+            const unsigned char *g = uniform_ptr((const unsigned char *)(g2 + ((size_t)((size_t)b * x_rows + first) * x_heads + x_head) * HD));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int row = 4 * i + ld_r;
+                lds_dma16(g, (uint32_t)min(row, last) * (uint32_t)(x_heads * ROW_BYTES) + ((ld_u ^ swz(row)) << 4),
+                          __builtin_amdgcn_readfirstlane(lds0 + X2_BASE + wave * (64 * ROW_BYTES) + i * 1024));
+            }
+        }
+    }
+    f32x16 acc1[NT][4], acc2[NT][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc1[t][d][r] = acc2[t][d][r] = 0.0f;
+
+    // ---- LDS read addresses within a tile: row l32, unit 2 s + hh; and, transposed, row 4 hh + i / 4 (+ 8, + 16) and four d's.
+    // Rows 16 apart have the same swizzle; rows 8 apart have units whose bit 1 differs.
+    int raddr[8], taddr[2][4];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) raddr[s] = l32 * ROW_BYTES + (((2 * s + hh) ^ swz(l32)) << 4);
+    {
+        const int i16 = lane & 15, g = (lane >> 4) & 1;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const int row = 8 * e + 4 * hh + (i16 >> 2), col = 32 * d + 16 * g + 4 * (i16 & 3);
+                taddr[e][d] = row * ROW_BYTES + (((col >> 3) ^ swz(row)) << 4) + (col & 7) * 2;
+            }
+    }
+    auto row_frag = [&](const LDS_AS unsigned char *tile_at, int s) __attribute__((always_inline)) -> bf16x8 {
+        return *(const LDS_AS bf16x8 *)(tile_at + raddr[s]);
+    };
+    auto col_frag = [&](const LDS_AS unsigned char *tile_at, int s, int d) __attribute__((always_inline)) -> bf16x8 {
+        s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile_at + taddr[0][d] + 16 * s * ROW_BYTES));
+        s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile_at + taddr[1][d] + 16 * s * ROW_BYTES));
+        s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        return __builtin_bit_cast(bf16x8, v);
+    };
+
+    // ---- the steps
+    const int x_last = min(x0 + 32 * NT, x_rows) - 1;
+    auto step = [&]() __attribute__((always_inline)) {
+        const int y0 = cur.tile * BT;
+        const bool masked = KEYS ? x_last > y0 + p.off : (y0 + BT - 1 > x0 + p.off || y0 + BT > y_rows);
+        const LDS_AS unsigned char *at = lds + cur.stage, *at2 = at + TILE_BYTES;
+        f32x16 s[NT], dp[NT];
+        f32x4 nlv[4];
+        f32x16 ndv;
+        if (KEYS) {
+            const LDS_AS unsigned char *st = at + 2 * TILE_BYTES + wave * STATS_BYTES;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                nlv[g] = *(const LDS_AS f32x4 *)(st + (8 * g + 4 * hh) * 4);
+                const f32x4 d = *(const LDS_AS f32x4 *)(st + BT * 4 + (8 * g + 4 * hh) * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ndv[4 * g + e] = d[e];
+            }
+        }
+        f32x16 zero;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const bf16x8 a = row_frag(at, k);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, x1[t][k], k == 0 ? zero : s[t], 0, 0, 0);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const bf16x8 a = row_frag(at2, k);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const bf16x8 x = X2_LDS ? row_frag(x2l + t * 32 * ROW_BYTES, k) : x2[t][k];
+                dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, x, k == 0 ? (KEYS ? ndv : nd[t]) : dp[t], 0, 0, 0);
+            }
+        }
+        // P and dS, rounded to BF16 for the products that follow: half a step of 2^-8 relative each, independent from element to
+        // element of sums over all rows or keys
+        uint32_t pb[NT][8], ds[NT][8];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], p.c, KEYS ? nlv[r >> 2][r & 3] : nl[t]));
+            if (masked) {
+                // KEYS: row >= key - off; else: key <= row + off and key < Skv.  A masked pair gives exactly 0, whatever it holds.
+                const int x = x0 + 32 * t + l32;
+                const int lim = (KEYS ? x - p.off : min(x + p.off, p.Skv - 1)) - y0 - 4 * hh;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int y = 8 * (r >> 2) + (r & 3);
+                    const bool ok = KEYS ? y >= lim : y <= lim;
+                    s[t][r] = ok ? s[t][r] : 0.0f;
+                    dp[t][r] = ok ? dp[t][r] : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                pb[t][r >> 1] = pack_bf16(s[t][r], s[t][r + 1]);
+                ds[t][r >> 1] = pack_bf16(s[t][r] * dp[t][r], s[t][r + 1] * dp[t][r + 1]);
+            }
+        }
+        auto half = [&](const uint32_t (&w)[8], int k) __attribute__((always_inline)) -> bf16x8 {
+            const u32x4 x = {w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]};
+            return __builtin_bit_cast(bf16x8, x);
+        };
+        if (KEYS) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const bf16x8 a = col_frag(at2, k, d);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) acc2[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, half(pb[t], k), acc2[t][d], 0, 0, 0);
+                }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const bf16x8 a = col_frag(at, k, d);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc1[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, half(ds[t], k), acc1[t][d], 0, 0, 0);
+            }
+    };
+    if (steps > 0) {
+        request();
+        request();
+        for (int j = 0; j < steps; ++j) {
+            // this step's tiles have landed (all but the newest PER_STEP requests), for every wavefront; and every wavefront is done with
+            // the stage that step j + 2 takes
+            __builtin_amdgcn_s_waitcnt(wait_vmcnt(PER_STEP));
+            wg_barrier();
+            request();
+            // (not where no pair of the step is valid for this wavefront: queries in front of its keys, keys behind its rows' last)
+            if (x0 < x_rows && (KEYS ? x0 <= cur.tile * BT + BT - 1 + p.off : cur.tile * BT <= x_last + p.off)) step();
+            next(cur);
+        }
+        __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+    }
+
+    // ---- results: lane = held row, registers 4 d's; exchanged with lane ^ 32, eight in line
+    const int splits = KEYS ? p.keys.splits : p.rows.splits;
+    auto store = [&](f32x16 (&acc)[NT][4], float f, __bf16 *out, float *part) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int row = x0 + 32 * t + l32;
+            const bool valid = row < x_rows;
+            const size_t at = ((size_t)((size_t)b * x_rows + (valid ? row : 0)) * x_heads + x_head) * HD;
+            if (splits == 1) {
+                unsigned char *op = (unsigned char *)(out + at + 8 * hh);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const f32x16 &a = acc[t][i >> 1];
+                    const int e = 8 * (i & 1);
+                    auto u = __builtin_amdgcn_permlane32_swap(pack_bf16(a[e] * f, a[e + 1] * f), pack_bf16(a[e + 4] * f, a[e + 5] * f), false, false);
+                    auto w = __builtin_amdgcn_permlane32_swap(pack_bf16(a[e + 2] * f, a[e + 3] * f), pack_bf16(a[e + 6] * f, a[e + 7] * f), false, false);
+                    const u32x4 ww = {u[0], w[0], u[1], w[1]};
+                    if (valid) *(u32x4 *)(op + 32 * i) = ww;
+                }
+            } else if (valid) {
+                float *op = part + at + 4 * hh;
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x16 &a = acc[t][d];
+                        const f32x4 y = {a[4 * g] * f, a[4 * g + 1] * f, a[4 * g + 2] * f, a[4 * g + 3] * f};
+                        *(f32x4 *)(op + 32 * d + 8 * g) = y;
+                    }
+            }
+        }
+    };
+    const size_t all = (size_t)p.B * x_rows * x_heads * HD;
+    if (KEYS) {
+        store(acc1, p.scale, p.dk, p.part_kv + (size_t)split * 2 * all);
+        store(acc2, 1.0f, p.dv, p.part_kv + ((size_t)split * 2 + 1) * all);
+    } else {
+        store(acc1, p.scale, p.dq, p.part_q + (size_t)split * all);
+    }
+}
+
+template <int NT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3 - NT, 3 - NT))) void attn_bwd_kernel(const Params p)
+{
+    int n = blockIdx.x;
+    if (n < p.rows.first) {
+        const int per = p.keys.groups * p.keys.splits;
+        const int tile = n / per;
+        n -= tile * per;
+        const int split = n / p.keys.groups;
+        item<true, NT>(p, n - split * p.keys.groups, tile, split);
+    } else {
+        n -= p.rows.first;
+        const int per = p.rows.groups * p.rows.splits;
+        const int tile = n / per;
+        n -= tile * per;
+        const int split = n / p.rows.groups;
+        item<false, NT>(p, n - split * p.rows.groups, p.rows.tiles - 1 - tile, split);
+    }
+}
+
+// Sum of the parts of an output, in the order of the parts.
+__global__ __launch_bounds__(256) void attn_bwd_join(const float *part, __bf16 *out, size_t n8, size_t stride, int splits)
+{
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n8) return;
+    f32x4 a = {0, 0, 0, 0}, c = {0, 0, 0, 0};
+    for (int s = 0; s < splits; ++s) {
+        const f32x4 *at = (const f32x4 *)(part + (size_t)s * stride) + 2 * i;
+        a += at[0];
+        c += at[1];
+    }
+    const u32x4 w = {pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(c[0], c[1]), pack_bf16(c[2], c[3])};
+    *((u32x4 *)out + i) = w;
+}
+
+// ----------------------------------------------------------------------------------------------------------- host
+struct Plan {
+    int nt, pack, chunks, qtiles;
+    Role keys, rows;
+    size_t stats, part_kv, part_q, total;       // bytes: the workspace's three parts
+};
+
+int check_sizes(int B, int Hq, int Hkv, int Sq, int Skv, int D)
+{
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Skv <= 0 || D <= 0) return ATTN_E_SHAPE;
+    if (Hq % Hkv != 0) return ATTN_E_SHAPE;
+    if (D != HD) return ATTN_E_UNSUPPORTED;
+    if ((long long)Sq + Skv >= (1ll << 31) - 1024 || Hq > 32768 || Hkv > 32768) return ATTN_E_UNSUPPORTED;
+    return ATTN_OK;
+}
+
+int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &r)
+{
+    const int G = Hq / Hkv;
+    r.pack = G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1;
+    r.chunks = G / r.pack;
+    r.qtiles = (Sq + BT - 1) / BT;
+    r.nt = 2;
+    const int pos = 128 * r.nt / r.pack, keys = 128 * r.nt;
+    r.keys = {B * Hkv, (Skv + keys - 1) / keys, 1, 0};
+    r.rows = {B * Hkv * r.chunks, (Sq + pos - 1) / pos, 1, 0};
+    const long long nk = (long long)r.keys.groups * r.keys.tiles * r.keys.splits, nr = (long long)r.rows.groups * r.rows.tiles * r.rows.splits;
+    r.rows.first = (int)nk;
+    if ((long long)B * Hkv * r.chunks >= (1ll << 24) || nk + nr >= (1ll << 24) || B > 65535 || (long long)r.qtiles * BT * Hq >= (1ll << 32) - 64)
+        return ATTN_E_UNSUPPORTED;
+    auto pad = [](size_t n) { return (n + 255) / 256 * 256; };
+    r.stats = pad((size_t)B * Hq * r.qtiles * 2 * BT * sizeof(float));
+    r.part_kv = r.keys.splits > 1 ? pad((size_t)r.keys.splits * 2 * B * Skv * Hkv * HD * sizeof(float)) : 0;
+    r.part_q = r.rows.splits > 1 ? pad((size_t)r.rows.splits * B * Sq * Hq * HD * sizeof(float)) : 0;
+    r.total = r.stats + r.part_kv + r.part_q;
+    return ATTN_OK;
+}
+
+bool launch(const void *kernel, dim3 grid, int threads, int lds, void **args, hipStream_t st)
+{
+    if (hipLaunchKernel(kernel, grid, dim3(threads), args, lds, st) == hipSuccess) return true;
+    (void)hipGetLastError();
+    return false;
+}
+
+}  // namespace
+
+extern "C" {
+
+long long attn_bwd_workspace(int B, int Hq, int Hkv, int Sq, int Skv, int D, int causal)
+{
+    int rc = check_sizes(B, Hq, Hkv, Sq, Skv, D);
+    Plan r = {};
+    if (rc == ATTN_OK) rc = make_plan(B, Hq, Hkv, Sq, Skv, causal, r);
+    return rc == ATTN_OK ? (long long)r.total : rc;
+}
+
+int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, const void *v, const void *o,
+             const float *lse, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes,
+             int B, int Hq, int Hkv, int Sq, int Skv, int D, int causal, float scale, void *stream)
+{
+    if (!dout || !q || !k || !v || !o || !lse || !dq || !dk || !dv || !workspace) return ATTN_E_NULL;
+    int rc = check_sizes(B, Hq, Hkv, Sq, Skv, D);
+    if (rc != ATTN_OK) return rc;
+    if (!isfinite(scale)) return ATTN_E_SCALE;
+    if (((uintptr_t)dout | (uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o | (uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv |
+         (uintptr_t)workspace) & 15)
+        return ATTN_E_ALIGN;
+    if (((uintptr_t)lse | (uintptr_t)dlse) & 3) return ATTN_E_ALIGN;
+    Plan r = {};
+    rc = make_plan(B, Hq, Hkv, Sq, Skv, causal, r);
+    if (rc != ATTN_OK) return rc;
+    if (workspace_bytes < r.total) return ATTN_E_WORKSPACE;
+
+    // Once per device: the opt-in that more than 64 KiB of dynamic LDS needs.
+    static std::atomic<bool> ready[64];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return ATTN_E_LAUNCH;
+    if (!ready[dev].load(std::memory_order_acquire)) {
+        if (hipFuncSetAttribute((const void *)attn_bwd_kernel<2>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(2)) != hipSuccess)
+            return ATTN_E_LAUNCH;
+        ready[dev].store(true, std::memory_order_release);
+    }
+    hipStream_t st = (hipStream_t)stream;
+
+    Params p = {};
+    p.q = (const __bf16 *)q; p.k = (const __bf16 *)k; p.v = (const __bf16 *)v; p.dout = (const __bf16 *)dout;
+    p.dq = (__bf16 *)dq; p.dk = (__bf16 *)dk; p.dv = (__bf16 *)dv;
+    p.stats = (const float *)workspace;
+    p.part_kv = (float *)((unsigned char *)workspace + r.stats);
+    p.part_q = (float *)((unsigned char *)workspace + r.stats + r.part_kv);
+    p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.Sq = Sq; p.Skv = Skv; p.G = Hq / Hkv; p.qtiles = r.qtiles;
+    p.pack = r.pack; p.chunks = r.chunks;
+    // (i + INT32_MAX - Sq - 256 is above every key for i >= 0 and within 32 bits for the i < Sq + 256 of a tile)
+    p.off = causal ? Skv - Sq : INT32_MAX - Sq - 256;
+    p.c = scale * LOG2E;
+    p.scale = scale;
+    p.keys = r.keys; p.rows = r.rows;
+
+    {
+        float *stats = (float *)workspace;
+        unsigned rows = (unsigned)r.qtiles * BT * (unsigned)Hq;
+        void *args[] = {(void *)&dout, (void *)&o, (void *)&lse, (void *)&dlse, &stats, &Hq, &Sq, &r.qtiles, &rows};
+        if (!launch((const void *)attn_bwd_stats, dim3((rows + 63) / 64, B), 256, 0, args, st)) return ATTN_E_LAUNCH;
+    }
+    {
+        void *args[] = {&p};
+        const int items = r.rows.first + r.rows.groups * r.rows.tiles * r.rows.splits;
+        if (!launch((const void *)attn_bwd_kernel<2>, dim3(items), 256, lds_bytes(2), args, st)) return ATTN_E_LAUNCH;
+    }
+    auto join = [&](const float *part, void *out, size_t n, size_t stride, int splits) -> bool {
+        size_t n8 = n / 8;
+        void *args[] = {&part, &out, &n8, &stride, &splits};
+        return launch((const void *)attn_bwd_join, dim3((unsigned)((n8 + 255) / 256)), 256, 0, args, st);
+    };
+    const size_t nq = (size_t)B * Sq * Hq * HD, nkv = (size_t)B * Skv * Hkv * HD;
+    if (r.keys.splits > 1 && !(join(p.part_kv, dk, nkv, 2 * nkv, r.keys.splits) && join(p.part_kv + nkv, dv, nkv, 2 * nkv, r.keys.splits)))
+        return ATTN_E_LAUNCH;
+    if (r.rows.splits > 1 && !join(p.part_q, dq, nq, nq, r.rows.splits)) return ATTN_E_LAUNCH;
+    return ATTN_OK;
+}
+
+}  // extern "C"

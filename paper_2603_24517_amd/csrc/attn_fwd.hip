@@ -2690,6 +2690,7 @@ const char *attn_strerror(int code)
     case ATTN_E_ALIGN:       return "misaligned pointer: q, k, v, o need 16-byte and lse 4-byte alignment";
     case ATTN_E_SCALE:       return "scale must be finite";
     case ATTN_E_LAUNCH:      return "kernel launch failed";
+    case ATTN_E_WORKSPACE:   return "workspace smaller than needed";
     default:                 return "unknown attn error code";
     }
 }

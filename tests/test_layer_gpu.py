@@ -1,0 +1,353 @@
+"""attention_backward, qk_norm_rope and qk_norm_rope_backward against 64-bit arithmetic (layer_util says how far they may be off)."""
+import math
+
+import pytest
+import torch
+
+import layer_util as L
+import paper_2603_24517_amd as A
+
+pytestmark = pytest.mark.gpu
+SCALE = 1.0 / math.sqrt(128)
+
+
+def cuda(*tensors):
+    return [None if t is None else t.cuda() for t in tensors]
+
+
+def inputs(B, Hq, Hkv, Sq, Skv, causal, seed, scale=SCALE, q_mul=1.0, do_mul=1.0, dlse=False):
+    q = L.rand(seed, B, Sq, Hq, 128, mul=q_mul)
+    k, v = L.rand(seed + 1, B, Skv, Hkv, 128), L.rand(seed + 2, B, Skv, Hkv, 128)
+    do = L.rand(seed + 3, B, Sq, Hq, 128, mul=do_mul)
+    o, lse = L.forward64(q, k, v, causal, scale)
+    dl = L.rand(seed + 4, B, Hq, Sq, mul=do_mul).float() if dlse else None
+    return do, q, k, v, o, lse, dl
+
+
+# B, Hq, Hkv, Sq, Skv, causal: one token; tile borders of 32, 64, 128, 256 rows; more queries than keys (rows without a key under the mask); fewer;
+# head groups of 1, 2, 3, 4, 6, 8
+SHAPES = [
+    (1, 1, 1, 1, 1, True), (2, 2, 1, 1, 1, False), (1, 4, 2, 1, 77, True), (3, 2, 2, 1, 600, False),
+    (1, 2, 2, 31, 31, True), (1, 2, 1, 32, 32, True), (2, 2, 2, 33, 33, True), (1, 2, 2, 33, 65, False),
+    (1, 4, 1, 64, 64, True), (1, 3, 1, 65, 63, False), (1, 6, 2, 100, 100, True), (2, 4, 4, 127, 129, True),
+    (1, 8, 1, 130, 130, True), (1, 2, 2, 255, 257, False), (1, 1, 1, 256, 256, True), (1, 1, 1, 257, 257, True),
+    (1, 2, 1, 300, 40, True), (1, 2, 2, 300, 1, True), (2, 2, 1, 70, 33, True), (1, 4, 4, 520, 520, True),
+    (1, 2, 1, 40, 700, True), (1, 8, 2, 17, 1030, True), (1, 2, 2, 600, 90, False), (1, 12, 2, 50, 200, True),
+    (5, 4, 2, 200, 200, True), (1, 32, 8, 96, 160, True), (1, 1, 1, 1500, 900, True), (1, 1, 1, 900, 1500, False),
+]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_backward(shape):
+    n = SHAPES.index(shape)
+    causal = shape[5]
+    do, q, k, v, o, lse, dl = inputs(*shape, seed=100 + 10 * n, dlse=n % 3 == 0, q_mul=2.0 if n % 4 == 1 else 1.0,
+                                     do_mul=2.0 ** -10 if n % 5 == 2 else 1.0)
+    d = cuda(do, q, k, v, o, lse, dl)
+    got = A.attention_backward(*d[:6], causal=causal, dlse=d[6])
+    assert [x.dtype for x in got] == [torch.bfloat16] * 3 and [x.shape for x in got] == [q.shape, k.shape, v.shape]
+    L.check_backward(got, L.backward64(do, q, k, v, o, lse, causal, SCALE, dl), str(shape))
+
+
+@pytest.mark.parametrize("scale", [-0.1, 0.0, 0.02, 0.5])
+@pytest.mark.parametrize("causal", [False, True])
+def test_backward_scales(scale, causal):
+    do, q, k, v, o, lse, _ = inputs(1, 4, 2, 90, 110, causal, seed=2000, scale=scale)
+    got = A.attention_backward(*cuda(do, q, k, v, o, lse), causal=causal, scale=scale)
+    L.check_backward(got, L.backward64(do, q, k, v, o, lse, causal, scale), f"scale {scale}")
+
+
+def test_backward_of_rows_without_a_key():
+    """Under the mask, with more queries than keys, the first rows see nothing: no gradient of theirs, whatever arrives."""
+    do, q, k, v, o, lse, dl = inputs(1, 2, 1, 170, 100, True, seed=2100, dlse=True)
+    assert torch.isneginf(lse[:, :, :70]).all()
+    got = A.attention_backward(*cuda(do, q, k, v, o, lse), causal=True, dlse=dl.cuda())
+    assert (got[0][:, :70] == 0).all()
+    L.check_backward(got, L.backward64(do, q, k, v, o, lse, True, SCALE, dl))
+    q2, do2 = q.clone(), do.clone()
+    q2[:, :40], do2[:, :40] = 7.0, -3.0         # rows that nothing sees
+    again = A.attention_backward(*cuda(do2, q2, k, v, o, lse), causal=True, dlse=dl.cuda())
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+def test_backward_of_large_and_small_scores():
+    """One dominant key per row, and rows whose probabilities all underflow but one."""
+    do, q, k, v, _, _, _ = inputs(1, 2, 2, 80, 80, True, seed=2200)
+    q = q * 16
+    k[:, ::7] *= 8
+    o, lse = L.forward64(q, k, v, True, SCALE)
+    got = A.attention_backward(*cuda(do, q, k, v, o, lse), causal=True)
+    # (arguments of the exponent reach 2^12 here, so FP32 leaves P 2^-24 * 2^12 relative: 2^4 times what the bound assumes)
+    ref, bound, terms = L.backward64(do, q, k, v, o, lse, True, SCALE)
+    L.check_backward(got, (ref, [b * (1 + 2.0 ** 4 * L.F / L.H) + 2.0 ** 4 * L.F * b / L.H for b in bound], [t * 2 for t in terms]))
+
+
+@pytest.mark.parametrize("shape", [(1, 8, 2, 1500, 1500, True), (2, 2, 2, 700, 1300, False), (1, 4, 1, 60, 9000, True), (1, 4, 4, 512, 512, False)],
+                         ids=str)
+def test_backward_same_bits_always(shape):
+    """Repeated, on another stream, and beside other launches; results of a call do not depend on what its memory held."""
+    do, q, k, v, o, lse, _ = cuda(*inputs(*shape, seed=2300))
+    first = A.attention_backward(do, q, k, v, o, lse, causal=shape[5])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    outs = []
+    for _ in range(3):
+        junk = torch.full((8 << 20,), float("nan"), device="cuda")
+        del junk
+        outs.append(A.attention_backward(do, q, k, v, o, lse, causal=shape[5]))
+        with torch.cuda.stream(side):
+            outs.append(A.attention_backward(do, q, k, v, o, lse, causal=shape[5]))
+    torch.cuda.synchronize()
+    for got in outs:
+        assert all(torch.equal(a, b) for a, b in zip(first, got))
+
+
+def test_backward_against_differences():
+    """The gradient of a number made of O and LSE against differences of the forward pass itself, along random directions."""
+    B, Hq, Hkv, S, causal = 1, 4, 2, 150, True
+    do, q, k, v, _, _, dl = inputs(B, Hq, Hkv, S, S, causal, seed=2400, dlse=True)
+    do, q, k, v, dl = cuda(do, q, k, v, dl)
+    o, lse = A.attention(q, k, v, causal=causal)
+    grads = A.attention_backward(do, q, k, v, o, lse, causal=causal, dlse=dl)
+
+    def value(q, k, v):
+        o, lse = L.forward64(q.cpu(), k.cpu(), v.cpu(), causal, SCALE)      # (O rounded: its error, H |O| per element, enters the tolerance)
+        return (do.cpu().double() * o.double()).sum().item() + (dl.cpu().double() * lse.double()).sum().item()
+
+    o_round = L.H * (do.double().square() * o.double().square()).sum().sqrt().item()
+    for n, x in enumerate((q, k, v)):
+        step = torch.where(torch.rand(x.shape, generator=torch.Generator().manual_seed(n)) < 0.5, -1, 1).cuda()
+        # one bit pattern up or down for every element: steps of half a unit in the last place, exactly representable on both sides
+        up, down = ((x.view(torch.int16) + s * step.to(torch.int16) * 4).view(torch.bfloat16) for s in (1, -1))
+        args = [q, k, v]
+        args[n] = up
+        hi = value(*args)
+        args[n] = down
+        lo = value(*args)
+        want = (grads[n].double() * (up.double() - down.double())).sum().item()
+        size = (grads[n].double() * (up.double() - down.double())).square().sum().sqrt().item()
+        # two rounded O's, 4-sigma; BF16 gradients, 4-sigma; second order: steps are 2^-5 relative, so a few per cent of the size
+        assert abs((hi - lo) - want) <= 4 * math.sqrt(2) * o_round + 4 * L.H * size + 0.1 * size * math.sqrt(8), (n, hi - lo, want)
+
+
+def test_backward_refuses():
+    do, q, k, v, o, lse, dl = cuda(*inputs(2, 4, 2, 20, 30, True, seed=2500, dlse=True))
+    good = dict(do=do, q=q, k=k, v=v, o=o, lse=lse, dlse=dl)
+    for name, bad in (("do", do.float()), ("do", do[:, :19]), ("do", do.transpose(1, 2)), ("do", do.cpu()), ("q", q.float()), ("q", q[0]),
+                      ("k", k[:, ::2]), ("k", k[:1]), ("v", v[:, 1:].contiguous()), ("o", o.transpose(1, 2).contiguous()), ("o", o.cpu()),
+                      ("lse", lse.double()), ("lse", lse[:, :2]), ("lse", lse.cpu()), ("dlse", dl.bfloat16()), ("dlse", dl.transpose(1, 2)),
+                      ("dlse", dl.cpu())):
+        with pytest.raises(ValueError):
+            A.attention_backward(**{**good, name: bad}, causal=True)
+    with pytest.raises(A.AttnError) as e:
+        A.attention_backward(**good, scale=math.inf)
+    assert e.value.code == A.ATTN_E_SCALE and "attn_bwd" in str(e.value)
+    with pytest.raises(A.AttnError) as e:
+        A.attention_backward(do, q, k[:, :, :1].expand(2, 30, 3, 128).contiguous(), v[:, :, :1].expand(2, 30, 3, 128).contiguous(), o, lse)
+    assert e.value.code == A.ATTN_E_SHAPE
+
+
+def _graph(call):
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = call()
+    return g, out
+
+
+@pytest.mark.parametrize("shape", [(1, 4, 2, 300, 300, True), (1, 2, 2, 64, 3000, True)], ids=str)
+def test_backward_in_a_graph(shape):
+    """Captured, replayed with other inputs in place, each replay against the call itself, with other work between."""
+    do, q, k, v, o, lse, _ = cuda(*inputs(*shape, seed=2600))
+    g, out = _graph(lambda: A.attention_backward(do, q, k, v, o, lse, causal=shape[5]))
+    for n in range(4):
+        do.copy_(L.rand(2700 + n, *do.shape))
+        g.replay()
+        torch.cuda.synchronize()
+        want = A.attention_backward(do, q, k, v, o, lse, causal=shape[5])
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), n
+
+
+# ------------------------------------------------------------------------------------------------- norm and rotation
+# B, S, Hq, Hkv, rotated, weight type, positions, interleaved, fused, with v
+ROPES = [
+    (1, 1, 1, 1, 128, torch.float32, None, False, False, False), (64, 1, 32, 8, 128, torch.bfloat16, torch.int64, False, True, True),
+    (3, 37, 4, 2, 64, torch.float32, torch.int32, False, True, True), (2, 5, 3, 3, 16, torch.bfloat16, None, True, False, True),
+    (1, 200, 5, 1, 96, None, torch.int64, True, True, True), (2, 33, 16, 16, 128, torch.float32, None, True, True, False),
+    (1, 7, 2, 5, 112, None, torch.int32, False, False, False), (5, 129, 8, 4, 32, torch.bfloat16, torch.int64, False, True, True),
+]
+
+
+def rope_inputs(B, S, Hq, Hkv, rotated, weight, positions, interleaved, fused, with_v, seed):
+    if fused:
+        q, k, v = L.rand(seed, B, S, Hq + 2 * Hkv, 128).split([Hq, Hkv, Hkv], dim=2)
+    else:
+        q, k, v = L.rand(seed, B, S, Hq, 128), L.rand(seed + 1, B, S, Hkv, 128), L.rand(seed + 2, B, S, Hkv, 128)
+    g = torch.Generator().manual_seed(seed + 3)
+    qw = kw = None
+    if weight is not None:
+        qw, kw = ((1 + 0.3 * torch.randn(128, generator=g)).to(weight) for _ in range(2))
+    cos, sin = L.table(300, rotated)
+    pos = None if positions is None else torch.randint(0, 300, (B, S), generator=g).to(positions)
+    return q, k, v if with_v else None, qw, kw, cos, sin, pos
+
+
+def on_device(t):
+    """The same strides on the device (slices of one projection stay that)."""
+    base = t.as_strided((t.untyped_storage().nbytes() // t.element_size(),), (1,), 0).cuda()
+    return base.as_strided(t.shape, t.stride(), t.storage_offset())
+
+
+@pytest.mark.parametrize("case", ROPES, ids=str)
+def test_norm_rope(case):
+    B, S = case[:2]
+    q, k, v, qw, kw, cos, sin, pos = rope_inputs(*case, seed=3000 + 10 * ROPES.index(case))
+    inter = case[7]
+    dev = [on_device(q), on_device(k), *cuda(qw, kw, cos, sin, pos)]
+    got = A.qk_norm_rope(*dev, eps=1e-5, interleaved=inter, v=None if v is None else on_device(v))
+    at = torch.arange(S).expand(B, S) if pos is None else pos.long()
+    for x, t, w, name in ((got[0], q, qw, "q"), (got[1], k, kw, "k")):
+        assert x.is_contiguous() and x.dtype == torch.bfloat16
+        L.check_close(x, L.norm_rope64(t, w, cos, sin, at, 1e-5, inter), f"{case} {name}")
+    assert len(got) == (2 if v is None else 3)
+    if v is not None:
+        assert got[2].is_contiguous() and torch.equal(got[2].cpu(), v.contiguous())
+
+
+@pytest.mark.parametrize("case", ROPES, ids=str)
+def test_norm_rope_backward(case):
+    B, S, Hq, Hkv = case[:4]
+    seed = 4000 + 10 * ROPES.index(case)
+    q, k, v, qw, kw, cos, sin, pos = rope_inputs(*case, seed=seed)
+    inter = case[7]
+    dq, dk, dv = L.rand(seed + 5, B, S, Hq, 128), L.rand(seed + 6, B, S, Hkv, 128), L.rand(seed + 7, B, S, Hkv, 128)
+    dev = [on_device(q), on_device(k), *cuda(qw, kw, cos, sin, pos)]
+    out = None
+    whole = torch.full((B, S, Hq + 2 * Hkv, 128), 9.0, dtype=torch.bfloat16, device="cuda")
+    if case[8]:
+        out = whole.split([Hq, Hkv, Hkv], dim=2)[:2 if v is None else 3]
+    got = A.qk_norm_rope_backward(dq.cuda(), dk.cuda(), *dev, eps=1e-5, interleaved=inter, dv=None if v is None else dv.cuda(), out=out)
+    at = torch.arange(S).expand(B, S) if pos is None else pos.long()
+    *dx, dqw, dkw = got
+    if out is not None:
+        assert all(a.data_ptr() == b.data_ptr() for a, b in zip(dx, out))
+        if v is None:
+            assert (whole[:, :, Hq + Hkv:] == 9.0).all()
+    for x, dw, dz, t, w, name in ((dx[0], dqw, dq, q, qw, "q"), (dx[1], dkw, dk, k, kw, "k")):
+        want_x, want_w = L.norm_rope_backward64(dz, t, w, cos, sin, at, 1e-5, inter)
+        L.check_close(x, want_x, f"{case} d{name}")
+        if w is None:
+            assert dw is None
+        else:
+            assert dw.dtype == torch.float32
+            L.check_close(dw, want_w, f"{case} d{name}_weight")
+    if v is not None:
+        assert torch.equal(dx[2].cpu(), dv)
+
+
+@pytest.mark.parametrize("strides", ["transposed", "every other", "broadcast", "cache"])
+def test_norm_rope_strides(strides):
+    """Heads before tokens, every other head, one head for all, and results into a slice of a cache with the rest left as it was."""
+    B, S, H = 2, 19, 4
+    cos, sin = L.table(40, 128)
+    out = cache = None
+    if strides == "transposed":
+        q = L.rand(1, B, H, S, 128).transpose(1, 2)
+    elif strides == "every other":
+        q = L.rand(2, B, S, 2 * H, 128)[:, :, ::2]
+    elif strides == "broadcast":
+        q = L.rand(3, B, S, 1, 128).expand(B, S, H, 128)
+    else:
+        q = L.rand(4, B, S, H, 128)
+        cache = [torch.full((B, 60, H, 128), 3.0, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+        out = [c[:, 20:20 + S] for c in cache]
+    k, v = L.rand(5, B, S, H, 128), L.rand(6, B, S, H, 128)
+    got = A.qk_norm_rope(on_device(q), k.cuda(), None, None, *cuda(cos, sin), v=v.cuda(), out=out)
+    at = torch.arange(S).expand(B, S)
+    L.check_close(got[0], L.norm_rope64(q, None, cos, sin, at, 1e-6, False), strides)
+    L.check_close(got[1], L.norm_rope64(k, None, cos, sin, at, 1e-6, False), strides)
+    assert torch.equal(got[2].cpu(), v)
+    if cache:
+        for c in cache:
+            assert (c[:, :20] == 3.0).all() and (c[:, 20 + S:] == 3.0).all()
+
+
+def test_norm_rope_places_outside_the_table():
+    q, k = L.rand(1, 1, 4, 2, 128).cuda(), L.rand(2, 1, 4, 1, 128).cuda()
+    cos, sin = cuda(*L.table(10, 128))
+    for dtype in (torch.int32, torch.int64):
+        pos = torch.tensor([[0, 10, -1, 9]], dtype=dtype, device="cuda")
+        for x in A.qk_norm_rope(q, k, None, None, cos, sin, pos):
+            assert torch.isnan(x[:, 1:3].float()).all() and not torch.isnan(x[:, ::3].float()).any()
+    pos = torch.tensor([[0, 1 << 40, 3, -(1 << 40)]], device="cuda")
+    x = A.qk_norm_rope(q, k, None, None, cos, sin, pos)[0]
+    assert torch.isnan(x[:, 1::2].float()).all() and not torch.isnan(x[:, ::2].float()).any()
+
+
+def test_norm_rope_zeros_and_extremes():
+    """Rows of zeros (with eps; their gradient is that of x / sqrt(eps)), and rows whose squares leave BF16's but not FP32's precision."""
+    q = torch.zeros(1, 3, 2, 128, dtype=torch.bfloat16)
+    q[:, 1] = 1e15
+    q[:, 2] = L.rand(9, 2, 128) * 2.0 ** -30
+    cos, sin = L.table(3, 128)
+    at = torch.arange(3)[None]
+    for eps in (1e-6, 1e-18):
+        got, _ = A.qk_norm_rope(q.cuda(), q.cuda(), None, None, *cuda(cos, sin), eps=eps)
+        L.check_close(got, L.norm_rope64(q, None, cos, sin, at, eps, False), f"eps {eps}")
+        dz = L.rand(10, 1, 3, 2, 128)
+        dx = A.qk_norm_rope_backward(dz.cuda(), dz.cuda(), q.cuda(), q.cuda(), None, None, *cuda(cos, sin), eps=eps)[0]
+        L.check_close(dx, L.norm_rope_backward64(dz, q, None, cos, sin, at, eps, False)[0], f"eps {eps}")
+
+
+def test_norm_rope_refuses():
+    q, k = L.rand(1, 2, 6, 4, 128).cuda(), L.rand(2, 2, 6, 2, 128).cuda()
+    cos, sin = cuda(*L.table(16, 64))
+    w = torch.ones(128, device="cuda")
+    pos = torch.zeros(2, 6, dtype=torch.int32, device="cuda")
+    good = dict(q=q, k=k, q_weight=w, k_weight=w, cos=cos, sin=sin, positions=pos)
+    bads = [("q", q.float()), ("q", q[0]), ("q", q.cpu()), ("k", k[:1]), ("k", k.cpu()), ("k", k.transpose(2, 3)), ("q_weight", None),
+            ("q_weight", w.bfloat16()), ("k_weight", w[:64]), ("k_weight", w.cpu()), ("cos", cos.double()), ("cos", cos[:, :16]),
+            ("sin", sin.t().contiguous().t()), ("sin", sin.cpu()), ("positions", pos.float()), ("positions", pos[:, :3]), ("positions", pos.cpu()),
+            ("v", q), ("v", k.float()), ("out", (q,)), ("out", (q, q)), ("out", (torch.empty_like(q[:, :, :1]).expand_as(q), k))]
+    for name, bad in bads:
+        with pytest.raises(ValueError):
+            A.qk_norm_rope(**{**good, name: bad})
+        if name not in ("v", "out"):
+            with pytest.raises(ValueError):
+                A.qk_norm_rope_backward(q, k, **{**good, name: bad})
+    for kw in (dict(dq=q.float()), dict(dk=q), dict(dv=q), dict(dv=k.cpu()), dict(out=(q,))):
+        with pytest.raises(ValueError):
+            A.qk_norm_rope_backward(**{**good, "dq": q, "dk": k, **kw})
+    for change, code in ((dict(cos=cos[:, :20].contiguous(), sin=sin[:, :20].contiguous()), A.ATTN_E_UNSUPPORTED), (dict(eps=-1.0), A.ATTN_E_SCALE),
+                         (dict(cos=cos[:3], sin=sin[:3], positions=None), A.ATTN_E_SHAPE),
+                         (dict(q=torch.zeros(2 * 6 * 4 * 128 + 8, dtype=torch.bfloat16, device="cuda")[4:-4].view(2, 6, 4, 128)), A.ATTN_E_ALIGN)):
+        with pytest.raises(A.AttnError) as e:
+            A.qk_norm_rope(**{**good, **change})
+        assert e.value.code == code
+
+
+def test_norm_rope_in_a_graph_and_on_another_stream():
+    case = (2, 50, 8, 2, 128, torch.float32, torch.int64, False, True, True)
+    q, k, v, qw, kw, cos, sin, pos = rope_inputs(*case, seed=5000)
+    q, k, v = on_device(q), on_device(k), on_device(v)
+    qw, kw, cos, sin, pos = cuda(qw, kw, cos, sin, pos)
+    dq, dk = L.rand(5001, *q.shape).cuda(), L.rand(5002, *k.shape).cuda()
+    both = lambda: (*A.qk_norm_rope(q, k, qw, kw, cos, sin, pos, v=v), *A.qk_norm_rope_backward(dq, dk, q, k, qw, kw, cos, sin, pos))
+    g, out = _graph(both)
+    for n in range(4):
+        dq.copy_(L.rand(5100 + n, *dq.shape))
+        pos.copy_((pos + 13) % 300)
+        g.replay()
+        torch.cuda.synchronize()
+        want = both()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), n
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = both()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(other, want))
