@@ -24,6 +24,7 @@
 #include <math.h>
 #include <atomic>
 #include <type_traits>
+#include <utility>
 
 #include "../../include/attn.h"
 #include "../../include/attn_layer.h"
@@ -44,13 +45,19 @@ constexpr int HD = 128;
 constexpr int ROW_BYTES = HD * 2;
 constexpr int BT = 32;                          // streamed rows per step
 constexpr int TILE_BYTES = BT * ROW_BYTES;      // 8 KiB
-constexpr int NSTAGE = 3;
 constexpr int STATS_BYTES = 2 * BT * 4;         // -LSE and -delta of a step's 32 rows
-constexpr int STAGE_BYTES = 2 * TILE_BYTES + 4 * STATS_BYTES;   // (each wavefront has the figures for itself)
-constexpr int X2_BASE = NSTAGE * STAGE_BYTES;   // keys items with NT = 2: V, 16 KiB per wavefront
+// LDS stages.  While step j runs, tiles j + 1 and j + 2 arrive, and Y1 of step j - 1 is still read; in rows items, where that is the end of a step,
+// a read of step j - 2's may be on its way when the request that takes its stage leaves.
+constexpr int stages(bool keys) { return keys ? 4 : 5; }
+constexpr int stage_bytes(bool keys) { return 2 * TILE_BYTES + (keys ? 4 * STATS_BYTES : 0); }      // (each wavefront has the figures for itself)
+constexpr int X2_BASE = stages(true) * stage_bytes(true);   // keys items: V, 8 * NT KiB per wavefront
 constexpr float LOG2E = 1.4426950408889634f;
 
-constexpr int lds_bytes(int nt) { return X2_BASE + (nt == 2 ? 4 * 64 * ROW_BYTES : 0); }
+constexpr int lds_bytes(int nt)
+{
+    const int keys = X2_BASE + 4 * nt * 32 * ROW_BYTES, rows = stages(false) * stage_bytes(false);
+    return keys > rows ? keys : rows;
+}
 
 struct Role {
     int groups, tiles, splits;      // items: groups x tiles x splits
@@ -67,6 +74,12 @@ struct Params {
     float c, scale;                 // c = scale * log2(e)
     Role keys, rows;
 };
+
+// f(0), f(1), ... f(N - 1) with constants (the unroller gives up on a loop of this size)
+template <int... I, class F>
+__device__ __forceinline__ void static_for(std::integer_sequence<int, I...>, F &&f) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void static_for(F &&f) { static_for(std::make_integer_sequence<int, N>{}, f); }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     bf16x2 p = __builtin_convertvector((f32x2){a, b}, bf16x2);   // v_cvt_pk_bf16_f32, nearest even
@@ -94,6 +107,15 @@ __device__ __forceinline__ void lds_dma4(const unsigned char *base, uint32_t vof
                  : "memory", "m0");
 }
 #pragma clang diagnostic pop
+// acc += A B for the sums that a wavefront keeps through all steps, in the accumulation half of the register file (the compiler, which
+// gives all products of a kernel one form or moves them between the halves as it sees fit, otherwise copies up to 300 registers a step).
+// It knows nothing of the instruction's timing, so: A and B are vector-ALU results no younger than two products, or LDS reads, for
+// which the compiler waits; nothing but the same kind of product reads `acc` until acc_ready(), and two into the same registers are 4 * NT products apart.
+__device__ __forceinline__ void mfma_acc(f32x16 &acc, bf16x8 a, bf16x8 b) {
+    asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+}
+// 16 passes at most, so 18 wait states between a product and another instruction that reads its result
+__device__ __forceinline__ void acc_ready(f32x16 &acc) { asm volatile("s_nop 15\n\ts_nop 3" : "+a"(acc)); }
 constexpr int wait_vmcnt(int n) { return 0x0F70 | n; }     // s_waitcnt vmcnt(n), n < 16
 __device__ __forceinline__ void wg_barrier() {
     __builtin_amdgcn_sched_barrier(0);
@@ -160,7 +182,7 @@ __global__ __launch_bounds__(256) void attn_bwd_stats(const __bf16 *dout, const 
 template <bool KEYS, int NT>
 __device__ __forceinline__ void item(const Params &p, int group, int tile, int split)
 {
-    constexpr bool X2_LDS = KEYS && NT == 2;    // K, V, dK and dV of 64 keys in registers would be 384, and the scores do not fit beside them
+    constexpr int NSTAGE = stages(KEYS), STAGE_BYTES = stage_bytes(KEYS);
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     LDS_AS unsigned char *lds = (LDS_AS unsigned char *)smem;
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
@@ -206,7 +228,7 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
     const uint32_t y_stride = (uint32_t)y_heads * ROW_BYTES;
     const unsigned char *y1 = (const unsigned char *)(KEYS ? p.q : p.k), *y2 = (const unsigned char *)(KEYS ? p.dout : p.v);
 
-    // ---- requests: 4 rows x 256 bytes per instruction, two of each tile per wavefront
+    // ---- requests: 4 rows x 256 bytes per instruction, two of each tile per wavefront (and, KEYS, its 256 bytes of figures)
     const int ld_r = lane >> 4, ld_u = lane & 15;
     // where requests and steps stand: streamed tile, query head of the group, LDS stage
     struct At { int tile, head, stage; };
@@ -216,48 +238,56 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
     req.tile = KEYS ? step0 - req.head * per_head + t0 : step0;
     req.stage = 0;
     cur = req;
+    auto next_stage = [&](int st) __attribute__((always_inline)) { return st == (NSTAGE - 1) * STAGE_BYTES ? 0 : st + STAGE_BYTES; };
     auto next = [&](At &a) __attribute__((always_inline)) {
         if (++a.tile == y_tiles) {
             a.tile = t0;
             ++a.head;
         }
-        a.stage = a.stage == (NSTAGE - 1) * STAGE_BYTES ? 0 : a.stage + STAGE_BYTES;
+        a.stage = next_stage(a.stage);
+    };
+    constexpr int PER_STEP = KEYS ? 5 : 4;
+    int row_off[2];                                 // this lane's place in a whole tile
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int row = (wave * 2 + i) * 4 + ld_r;
+        row_off[i] = row * y_stride + ((ld_u ^ swz(row)) << 4);
+    }
+    // part n of the requests for a step
+    auto request_part = [&](int n) __attribute__((always_inline)) {
+        if (n < 4) {
+            const int i = n & 1;
+            const size_t at = ((size_t)((size_t)b * y_rows + (size_t)req.tile * BT) * y_heads + y_head0 + req.head) * ROW_BYTES;
+            uint32_t o = row_off[i];
+            const int last = y_rows - 1 - req.tile * BT;
+            if (last < BT - 1) {                    // rows past the end read the last one again
+                const int row = (wave * 2 + i) * 4 + ld_r;
+                o = (uint32_t)min(row, last) * y_stride + ((ld_u ^ swz(row)) << 4);
+            }
+            lds_dma16(uniform_ptr((n < 2 ? y1 : y2) + at), o,
+                      __builtin_amdgcn_readfirstlane(lds0 + req.stage + wave * 2048 + (n < 2 ? 0 : TILE_BYTES) + i * 1024));
+        } else {
+            const float *st = p.stats + ((size_t)((size_t)b * p.Hq + y_head0 + req.head) * p.qtiles + req.tile) * (2 * BT);
+            lds_dma4(uniform_ptr((const unsigned char *)st), lane * 4,
+                     __builtin_amdgcn_readfirstlane(lds0 + req.stage + 2 * TILE_BYTES + wave * STATS_BYTES));
+        }
     };
     // past the end the last step's tiles are read again, into stages that nobody reads, so that the number in flight stays the same
     int left = steps;
-    auto request = [&]() __attribute__((always_inline)) {
-        const int s = req.tile, head = req.head;
-        const int stage = req.stage;
-        const size_t at = ((size_t)((size_t)b * y_rows + (size_t)s * BT) * y_heads + y_head0 + head) * ROW_BYTES;
-        const unsigned char *g1 = uniform_ptr(y1 + at), *g2 = uniform_ptr(y2 + at);
-        const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + stage + wave * 2048);
-        const int last = y_rows - 1 - s * BT;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = (wave * 2 + i) * 4 + ld_r;
-            const uint32_t o = (uint32_t)min(row, last) * y_stride + ((ld_u ^ swz(row)) << 4);
-            lds_dma16(g1, o, to + i * 1024);
-            lds_dma16(g2, o, to + TILE_BYTES + i * 1024);
-        }
-        if (KEYS) {
-            const float *st = p.stats + ((size_t)((size_t)b * p.Hq + y_head0 + head) * p.qtiles + s) * (2 * BT);
-            lds_dma4(uniform_ptr((const unsigned char *)st), lane * 4,
-                     __builtin_amdgcn_readfirstlane(lds0 + stage + 2 * TILE_BYTES + wave * STATS_BYTES));
-        }
-        const int tile = req.tile, h = req.head;
+    auto request_done = [&]() __attribute__((always_inline)) {
+        const At was = req;
         next(req);
         if (--left <= 0) {
-            req.tile = tile;
-            req.head = h;
+            req.tile = was.tile;
+            req.head = was.head;
         }
     };
-    constexpr int PER_STEP = KEYS ? 5 : 4;
 
     // ---- held operands
     bf16x8 x1[NT][8], x2[NT][8];
     f32x16 nd[NT];              // rows items: -delta of the lane's row in every element, the C operand that dP starts from
     float nl[NT];
-    const LDS_AS unsigned char *x2l = lds + X2_BASE + wave * (64 * ROW_BYTES);
+    const LDS_AS unsigned char *x2l = lds + X2_BASE + wave * (NT * 32 * ROW_BYTES);
     {
         const __bf16 *g1 = KEYS ? p.k : p.q, *g2 = KEYS ? p.v : p.dout;
 #pragma unroll
@@ -266,11 +296,9 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
             const size_t at = ((size_t)((size_t)b * x_rows + row) * x_heads + x_head) * HD + 8 * hh;
 #pragma unroll
             for (int s = 0; s < 8; ++s) x1[t][s] = *(const bf16x8 *)(g1 + at + 16 * s);
-            if (!X2_LDS) {
+            if (!KEYS) {
 #pragma unroll
                 for (int s = 0; s < 8; ++s) x2[t][s] = *(const bf16x8 *)(g2 + at + 16 * s);
-            }
-            if (!KEYS) {
                 const int i = min(x0 + 32 * t + l32, p.Sq - 1);
                 const float *st = p.stats + ((size_t)((size_t)b * p.Hq + x_head) * p.qtiles + (i >> 5)) * (2 * BT) + (i & 31);
                 nl[t] = st[0];
@@ -279,14 +307,14 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
                 for (int r = 0; r < 16; ++r) nd[t][r] = d;
             }
         }
-        if (X2_LDS) {
+        if (KEYS) {             // (V in registers as well: no room beside K, two accumulators of its size and the scores)
             const int first = min(x0, x_rows - 1), last = x_rows - 1 - first;
             const unsigned char *g = uniform_ptr((const unsigned char *)(g2 + ((size_t)((size_t)b * x_rows + first) * x_heads + x_head) * HD));
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < 8 * NT; ++i) {
                 const int row = 4 * i + ld_r;
                 lds_dma16(g, (uint32_t)min(row, last) * (uint32_t)(x_heads * ROW_BYTES) + ((ld_u ^ swz(row)) << 4),
-                          __builtin_amdgcn_readfirstlane(lds0 + X2_BASE + wave * (64 * ROW_BYTES) + i * 1024));
+                          __builtin_amdgcn_readfirstlane(lds0 + X2_BASE + wave * (NT * 32 * ROW_BYTES) + i * 1024));
             }
         }
     }
@@ -298,133 +326,199 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc1[t][d][r] = acc2[t][d][r] = 0.0f;
 
-    // ---- LDS read addresses within a tile: row l32, unit 2 s + hh; and, transposed, row 4 hh + i / 4 (+ 8, + 16) and four d's.
-    // Rows 16 apart have the same swizzle; rows 8 apart have units whose bit 1 differs.
-    int raddr[8], taddr[2][4];
-#pragma unroll
-    for (int s = 0; s < 8; ++s) raddr[s] = l32 * ROW_BYTES + (((2 * s + hh) ^ swz(l32)) << 4);
+    // ---- LDS reads.  Row l32, unit 2 s + hh: as the swizzle is an exclusive or and tiles are 256-byte aligned, that is the address of
+    // unit hh with s << 5 flipped.  Transposed: row 4 hh + i / 4 (+ 8 e, + 16 k) and four d's: likewise with d << 6 and e << 5 flipped.
+    const uint32_t r_at = l32 * ROW_BYTES + ((hh ^ swz(l32)) << 4);
+    uint32_t t_at;
     {
-        const int i16 = lane & 15, g = (lane >> 4) & 1;
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                const int row = 8 * e + 4 * hh + (i16 >> 2), col = 32 * d + 16 * g + 4 * (i16 & 3);
-                taddr[e][d] = row * ROW_BYTES + (((col >> 3) ^ swz(row)) << 4) + (col & 7) * 2;
-            }
+        const int i16 = lane & 15, g = (lane >> 4) & 1, row = 4 * hh + (i16 >> 2), col = 16 * g + 4 * (i16 & 3);
+        t_at = row * ROW_BYTES + (((col >> 3) ^ swz(row)) << 4) + (col & 7) * 2;
     }
-    auto row_frag = [&](const LDS_AS unsigned char *tile_at, int s) __attribute__((always_inline)) -> bf16x8 {
-        return *(const LDS_AS bf16x8 *)(tile_at + raddr[s]);
+    typedef const LDS_AS unsigned char *Lds;
+    auto row_frag = [&](uint32_t at, int s, int imm) __attribute__((always_inline)) -> bf16x8 {     // `at`: r_at in the stage
+        return *(const LDS_AS bf16x8 *)((Lds)(uintptr_t)(at ^ (s << 5)) + imm);
     };
-    auto col_frag = [&](const LDS_AS unsigned char *tile_at, int s, int d) __attribute__((always_inline)) -> bf16x8 {
-        s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile_at + taddr[0][d] + 16 * s * ROW_BYTES));
-        s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile_at + taddr[1][d] + 16 * s * ROW_BYTES));
+    auto col_frag = [&](uint32_t at, int k, int d, int imm) __attribute__((always_inline)) -> bf16x8 {     // `at`: t_at in the stage
+        s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Lds)(uintptr_t)(at ^ (d << 6)) + (imm + 16 * k * ROW_BYTES)));
+        s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Lds)(uintptr_t)(at ^ (d << 6) ^ 32) + (imm + (16 * k + 8) * ROW_BYTES)));
         s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
         return __builtin_bit_cast(bf16x8, v);
     };
 
-    // ---- the steps
+    // ---- a step: phases of 8 operand fragments of Y, each fragment for NT products,
+    //     KEYS:  S(j)   acc1 += Y1^T dS(j-1)   dP(j)   acc2 += Y2^T P(j)
+    //     rows:  S(j)   dP(j)   acc1 += Y1^T dS(j-1)
+    // and between the products the vector work, each piece a phase or two after the products that it needs: rounding dS(j-1) during S(j), the
+    // exponents of S(j) during the two phases after it, P * dP behind dP(j).  Fragments are read LEAD ahead, across the end of
+    // a step too, so the step's barrier stands LEAD fragments before its end.
+    constexpr int LEAD = 3, LEAD2 = 2;
+    constexpr int NF = KEYS ? 32 : 24;          // fragments of a step
+    constexpr int PH_S = 0, PH_DP = KEYS ? 2 : 1, PH_1 = KEYS ? 1 : 2, PH_2 = 3;
+    constexpr int SLOTS = 8 * NT;               // products of a phase
+    bf16x8 frag[LEAD + 1], frag2[LEAD2 + 1][NT];
+    f32x16 s[NT], dp[NT];
+    uint32_t pb[NT][8], ds[NT][8];
+    int stage1 = 0;                             // stage of step j - 1
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[t][r] = 0.0f;
+    auto half = [&](const uint32_t (&w)[8], int k) __attribute__((always_inline)) -> bf16x8 {
+        const u32x4 x = {w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]};
+        return __builtin_bit_cast(bf16x8, x);
+    };
+    auto fetch = [&](int f, uint32_t at, uint32_t at1, uint32_t at_next) __attribute__((always_inline)) {    // stages of steps j, j - 1, j + 1
+        const int ph = (f % NF) >> 3, i = f & 7;
+        bf16x8 &to = frag[f % (LEAD + 1)];
+        if (f >= NF) to = row_frag(lds0 + at_next + r_at, i, 0);
+        else if (ph == PH_S) to = row_frag(lds0 + at + r_at, i, 0);
+        else if (ph == PH_DP) to = row_frag(lds0 + at + r_at, i, TILE_BYTES);
+        else if (ph == PH_1) to = col_frag(lds0 + at1 + t_at, i >> 2, i & 3, 0);
+        else to = col_frag(lds0 + at + t_at, i >> 2, i & 3, TILE_BYTES);
+    };
+    auto fetch2 = [&](int f) __attribute__((always_inline)) {
+        const int i = f & 7;
+        if (KEYS && f < NF && (f >> 3) == PH_DP) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) frag2[i % (LEAD2 + 1)][t] = row_frag((uint32_t)(uintptr_t)x2l + r_at, i, t * 32 * ROW_BYTES);
+        }
+    };
     const int x_last = min(x0 + 32 * NT, x_rows) - 1;
     auto step = [&]() __attribute__((always_inline)) {
         const int y0 = cur.tile * BT;
         const bool masked = KEYS ? x_last > y0 + p.off : (y0 + BT - 1 > x0 + p.off || y0 + BT > y_rows);
-        const LDS_AS unsigned char *at = lds + cur.stage, *at2 = at + TILE_BYTES;
-        f32x16 s[NT], dp[NT];
+        const uint32_t at = cur.stage, at1 = stage1, at_next = next_stage(cur.stage);
         f32x4 nlv[4];
-        f32x16 ndv;
-        if (KEYS) {
-            const LDS_AS unsigned char *st = at + 2 * TILE_BYTES + wave * STATS_BYTES;
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                nlv[g] = *(const LDS_AS f32x4 *)(st + (8 * g + 4 * hh) * 4);
-                const f32x4 d = *(const LDS_AS f32x4 *)(st + BT * 4 + (8 * g + 4 * hh) * 4);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) ndv[4 * g + e] = d[e];
-            }
-        }
-        f32x16 zero;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const bf16x8 a = row_frag(at, k);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, x1[t][k], k == 0 ? zero : s[t], 0, 0, 0);
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const bf16x8 a = row_frag(at2, k);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const bf16x8 x = X2_LDS ? row_frag(x2l + t * 32 * ROW_BYTES, k) : x2[t][k];
-                dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, x, k == 0 ? (KEYS ? ndv : nd[t]) : dp[t], 0, 0, 0);
-            }
-        }
-        // P and dS, rounded to BF16 for the products that follow: half a step of 2^-8 relative each, independent from element to
-        // element of sums over all rows or keys
-        uint32_t pb[NT][8], ds[NT][8];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                s[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], p.c, KEYS ? nlv[r >> 2][r & 3] : nl[t]));
+        // Masked pairs (KEYS: row < key - off; else key > row + off or key >= Skv) give exactly 0, whatever they hold.  A branch around
+        // selects alone: two forms of the whole step meet in copies of hundreds of registers.
+        auto mask = [&](auto &&f) __attribute__((always_inline)) {
             if (masked) {
-                // KEYS: row >= key - off; else: key <= row + off and key < Skv.  A masked pair gives exactly 0, whatever it holds.
-                const int x = x0 + 32 * t + l32;
-                const int lim = (KEYS ? x - p.off : min(x + p.off, p.Skv - 1)) - y0 - 4 * hh;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int y = 8 * (r >> 2) + (r & 3);
-                    const bool ok = KEYS ? y >= lim : y <= lim;
-                    s[t][r] = ok ? s[t][r] : 0.0f;
-                    dp[t][r] = ok ? dp[t][r] : 0.0f;
+                for (int t = 0; t < NT; ++t) {
+                    int ln = lane;
+                    asm volatile("" : "+v"(ln));        // formed here, not kept through all steps
+                    const int x = x0 + 32 * t + (ln & 31);
+                    const int lim = (KEYS ? x - p.off : min(x + p.off, p.Skv - 1)) - y0 - 4 * (ln >> 5);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int y = 8 * (r >> 2) + (r & 3);
+                        f(t, r, KEYS ? y >= lim : y <= lim);
+                    }
                 }
             }
-#pragma unroll
-            for (int r = 0; r < 16; r += 2) {
-                pb[t][r >> 1] = pack_bf16(s[t][r], s[t][r + 1]);
-                ds[t][r >> 1] = pack_bf16(s[t][r] * dp[t][r], s[t][r + 1] * dp[t][r + 1]);
-            }
-        }
-        auto half = [&](const uint32_t (&w)[8], int k) __attribute__((always_inline)) -> bf16x8 {
-            const u32x4 x = {w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]};
-            return __builtin_bit_cast(bf16x8, x);
+            __builtin_amdgcn_sched_barrier(0);
         };
-        if (KEYS) {
+        // element e of the vector work
+        auto do_round = [&](int e) __attribute__((always_inline)) {       // dS(j-1), pairs
+            const int t = e >> 3, r = 2 * (e & 7);
+            ds[t][e & 7] = pack_bf16(dp[t][r], dp[t][r + 1]);
+        };
+        auto do_exp = [&](int e) __attribute__((always_inline)) {
+            const int t = e >> 4, r = e & 15;
+            s[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], p.c, KEYS ? nlv[r >> 2][r & 3] : nl[t]));
+            if (KEYS && (r & 1)) pb[t][r >> 1] = pack_bf16(s[t][r - 1], s[t][r]);
+        };
+        auto do_mul = [&](int e) __attribute__((always_inline)) {
+            const int t = e >> 4, r = e & 15;
+            dp[t][r] = s[t][r] * dp[t][r];
+        };
+        // pieces lo .. hi of n that belong to slot `k` of `of`
+        auto spread = [&](int k, int of, int n, auto &&f) __attribute__((always_inline)) {
+            if (k < 0 || k >= of) return;
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const bf16x8 a = col_frag(at2, k, d);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) acc2[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, half(pb[t], k), acc2[t][d], 0, 0, 0);
-                }
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                const bf16x8 a = col_frag(at, k, d);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) acc1[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, half(ds[t], k), acc1[t][d], 0, 0, 0);
+            for (int e = 0; e < n; ++e)
+                if (e >= k * n / of && e < (k + 1) * n / of) f(e);
+        };
+        static_for<NF>([&](auto fc) __attribute__((always_inline)) {
+            constexpr int f = decltype(fc)::value, ph = f >> 3, i = f & 7;
+            if constexpr (KEYS && f == 8 * PH_2) {
+                mask([&](int t, int r, bool ok) __attribute__((always_inline)) {
+                    s[t][r] = ok ? s[t][r] : 0.0f;
+                    if (r & 1) pb[t][r >> 1] = pack_bf16(s[t][r - 1], s[t][r]);
+                });
             }
+            if (f == NF - LEAD) {
+                // the next step's tiles have landed (all but the newest PER_STEP requests), for every wavefront
+                __builtin_amdgcn_s_waitcnt(wait_vmcnt(PER_STEP));
+                wg_barrier();
+            }
+            fetch(f + LEAD, at, at1, at_next);
+            fetch2(f + LEAD2);
+            if (f >= 1 && f <= PER_STEP) request_part(f - 1);
+            if (f == PER_STEP + 1) request_done();
+            if constexpr (KEYS && f >= 4 && f < 8)
+                nlv[f - 4] = *(const LDS_AS f32x4 *)(lds + at + 2 * TILE_BYTES + wave * STATS_BYTES + (8 * (f - 4) + 4 * hh) * 4);
+            if constexpr (KEYS && f >= 8 && f < 12) {
+                const f32x4 d = *(const LDS_AS f32x4 *)(lds + at + 2 * TILE_BYTES + wave * STATS_BYTES + BT * 4 + (8 * (f - 8) + 4 * hh) * 4);
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dp[t][4 * (f - 8) + e] = d[e];
+            }
+            const bf16x8 a = frag[f % (LEAD + 1)];
+            static_for<NT>([&](auto tc) __attribute__((always_inline)) {
+                constexpr int t = decltype(tc)::value;
+                if constexpr (ph == PH_S) {
+                    f32x16 zero;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, x1[t][i], i == 0 ? zero : s[t], 0, 0, 0);
+                } else if constexpr (ph == PH_DP) {
+                    dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, KEYS ? frag2[i % (LEAD2 + 1)][t] : x2[t][i], !KEYS && i == 0 ? nd[t] : dp[t], 0, 0, 0);
+                } else if constexpr (ph == PH_1) {
+                    mfma_acc(acc1[t][i & 3], a, half(ds[t], i >> 2));
+                } else {
+                    mfma_acc(acc2[t][i & 3], a, half(pb[t], i >> 2));
+                }
+                constexpr int slot = f * NT + t;
+                spread(slot, SLOTS, 8 * NT, do_round);
+                if (KEYS) {
+                    spread(slot - SLOTS - NT, 2 * SLOTS - NT, 16 * NT, do_exp);
+                    spread(slot - 3 * SLOTS - NT, SLOTS - NT, 16 * NT, do_mul);
+                } else {
+                    spread(slot - SLOTS - NT, SLOTS + SLOTS / 2 - NT, 16 * NT, do_exp);
+                    spread(slot - 2 * SLOTS - NT, SLOTS - NT, 16 * NT, do_mul);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+        mask([&](int t, int r, bool ok) __attribute__((always_inline)) { dp[t][r] = ok ? dp[t][r] : 0.0f; });
+        stage1 = cur.stage;
+        next(cur);
     };
     if (steps > 0) {
-        request();
-        request();
-        for (int j = 0; j < steps; ++j) {
-            // this step's tiles have landed (all but the newest PER_STEP requests), for every wavefront; and every wavefront is done with
-            // the stage that step j + 2 takes
-            __builtin_amdgcn_s_waitcnt(wait_vmcnt(PER_STEP));
-            wg_barrier();
-            request();
-            // (not where no pair of the step is valid for this wavefront: queries in front of its keys, keys behind its rows' last)
-            if (x0 < x_rows && (KEYS ? x0 <= cur.tile * BT + BT - 1 + p.off : cur.tile * BT <= x_last + p.off)) step();
-            next(cur);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int n = 0; n < PER_STEP; ++n) request_part(n);
+            request_done();
         }
+        __builtin_amdgcn_s_waitcnt(wait_vmcnt(PER_STEP));
+        wg_barrier();
+#pragma unroll
+        for (int f = 0; f < LEAD; ++f) fetch(f, 0, 0, 0);
+        for (int j = 0; j < steps; ++j) step();
         __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+        // the last step's dS
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) ds[t][r >> 1] = pack_bf16(dp[t][r], dp[t][r + 1]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bf16x8 a = col_frag(lds0 + stage1 + t_at, i >> 2, i & 3, 0);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mfma_acc(acc1[t][i & 3], a, half(ds[t], i >> 2));
+        }
     }
 
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            acc_ready(acc1[t][d]);
+            if (KEYS) acc_ready(acc2[t][d]);
+        }
     // ---- results: lane = held row, registers 4 d's; exchanged with lane ^ 32, eight in line
     const int splits = KEYS ? p.keys.splits : p.rows.splits;
     auto store = [&](f32x16 (&acc)[NT][4], float f, __bf16 *out, float *part) __attribute__((always_inline)) {
