@@ -59,9 +59,13 @@ constexpr int lds_bytes(int nt)
     return keys > rows ? keys : rows;
 }
 
+// The items of one kind.  A tile's steps (streamed tiles, of all heads of a group) are cut into pieces of at most `most`, so that a call of few or
+// uneven tiles fills the chip; a tile of several pieces leaves FP32 parts, which attn_bwd_join adds up.
 struct Role {
-    int groups, tiles, splits;      // items: groups x tiles x splits
-    int first;                      // number of its first item
+    int groups, tiles, splits;      // grid: groups x tiles x splits (the largest number of pieces)
+    int most;
+    int window;                     // groups of an XCD whose tiles are dealt out together; 0: XCDs are not told apart
+    int items;
 };
 struct Params {
     const __bf16 *q, *k, *v, *dout;
@@ -80,6 +84,20 @@ template <int... I, class F>
 __device__ __forceinline__ void static_for(std::integer_sequence<int, I...>, F &&f) { (f(std::integral_constant<int, I>{}), ...); }
 template <int N, class F>
 __device__ __forceinline__ void static_for(F &&f) { static_for(std::make_integer_sequence<int, N>{}, f); }
+
+// Query tiles in front of a tile's first key (keys items); steps of a tile.
+__host__ __device__ inline int keys_skip(const Params &p, int tile, int nt)
+{
+    const int first = tile * (128 * nt) - p.off;        // first row that sees the tile's first key
+    return first > 0 ? (first / BT < p.qtiles ? first / BT : p.qtiles) : 0;
+}
+__host__ __device__ inline int rows_steps(const Params &p, int tile, int nt)
+{
+    const int end = (tile + 1) * (128 * nt / p.pack);
+    const int last = (end < p.Sq ? end : p.Sq) - 1 + p.off;      // last key that the tile's last row sees
+    return last < 0 ? 0 : (last < p.Skv - 1 ? last : p.Skv - 1) / BT + 1;
+}
+__host__ __device__ inline int pieces(int steps, int most) { return steps <= most ? 1 : (steps + most - 1) / most; }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     bf16x2 p = __builtin_convertvector((f32x2){a, b}, bf16x2);   // v_cvt_pk_bf16_f32, nearest even
@@ -180,7 +198,7 @@ __global__ __launch_bounds__(256) void attn_bwd_stats(const __bf16 *dout, const 
 // ------------------------------------------------------------------------------------------------------ the products
 // One item: KEYS holds K (X1), V (X2) and streams Q (Y1), dO (Y2); otherwise the reverse.  NT: held 32-row tiles per wavefront.
 template <bool KEYS, int NT>
-__device__ __forceinline__ void item(const Params &p, int group, int tile, int split)
+__device__ __forceinline__ void item(const Params &p, int group, int tile, int piece)
 {
     constexpr int NSTAGE = stages(KEYS), STAGE_BYTES = stage_bytes(KEYS);
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -190,7 +208,7 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
     // ---- what this wavefront holds, and the steps that it streams
-    int b, x_head, x0, x_rows, y_rows, y_head0, steps, step0;
+    int b, x_head, x0, x_rows, y_rows, y_head0;
     if (KEYS) {
         b = group / p.Hkv;
         x_head = group - b * p.Hkv;
@@ -207,79 +225,74 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
         x_rows = p.Sq;
         y_rows = p.Skv;
     }
-    // KEYS: query tiles t0 .. qtiles - 1 of each head; else: key tiles 0 .. t1 - 1
-    int t0 = 0, per_head;
-    if (KEYS) {
-        const int first = tile * (128 * NT) - p.off;        // first row that sees the item's first key
-        t0 = first > 0 ? min(first / BT, p.qtiles) : 0;
-        per_head = p.qtiles - t0;
-        steps = per_head * p.G;
-    } else {
-        const int last = min((tile + 1) * (128 * NT / p.pack), p.Sq) - 1 + p.off;      // last key that the item's last row sees
-        steps = last < 0 ? 0 : min(last / BT, (p.Skv - 1) / BT) + 1;
-        per_head = steps;
-    }
-    {
-        const int splits = KEYS ? p.keys.splits : p.rows.splits;
-        step0 = (int)((long long)steps * split / splits);
-        steps = (int)((long long)steps * (split + 1) / splits) - step0;
-    }
+    // KEYS: query tiles t0 .. qtiles - 1 of each head; else: key tiles from 0 on
+    const int t0 = KEYS ? keys_skip(p, tile, NT) : 0;
+    const int per_head = KEYS ? p.qtiles - t0 : rows_steps(p, tile, NT);
+    const int tile_steps = KEYS ? per_head * p.G : per_head, n_pieces = pieces(tile_steps, KEYS ? p.keys.most : p.rows.most);
+    if (piece >= n_pieces) return;
+    const int step0 = (int)((long long)tile_steps * piece / n_pieces);
+    int steps = (int)((long long)tile_steps * (piece + 1) / n_pieces) - step0;
+    // (all of it is wave-uniform: scalar registers)
+    auto uniform = [](int &x) __attribute__((always_inline)) { x = __builtin_amdgcn_readfirstlane(x); };
+    uniform(b); uniform(x_head); uniform(x0); uniform(y_head0); uniform(steps);
     const int x_heads = KEYS ? p.Hkv : p.Hq, y_heads = KEYS ? p.Hq : p.Hkv;
     const uint32_t y_stride = (uint32_t)y_heads * ROW_BYTES;
-    const unsigned char *y1 = (const unsigned char *)(KEYS ? p.q : p.k), *y2 = (const unsigned char *)(KEYS ? p.dout : p.v);
 
     // ---- requests: 4 rows x 256 bytes per instruction, two of each tile per wavefront (and, KEYS, its 256 bytes of figures)
     const int ld_r = lane >> 4, ld_u = lane & 15;
-    // where requests and steps stand: streamed tile, query head of the group, LDS stage
+    // Where steps and requests stand: streamed tile, query head of the group, LDS stage; and, for requests, the tiles' addresses.
     struct At { int tile, head, stage; };
-    const int y_tiles = KEYS ? p.qtiles : INT32_MAX;
-    At req, cur;
-    req.head = KEYS && per_head > 0 ? step0 / per_head : 0;
-    req.tile = KEYS ? step0 - req.head * per_head + t0 : step0;
-    req.stage = 0;
-    cur = req;
+    const int y_tiles = KEYS ? p.qtiles : (y_rows + BT - 1) / BT;
+    At cur, req;
+    cur.head = KEYS && per_head > 0 ? step0 / per_head : 0;
+    cur.tile = KEYS ? min(step0 - cur.head * per_head + t0, y_tiles - 1) : min(step0, y_tiles - 1);
+    uniform(cur.head);
+    uniform(cur.tile);
+    cur.stage = 0;
+    req = cur;
     auto next_stage = [&](int st) __attribute__((always_inline)) { return st == (NSTAGE - 1) * STAGE_BYTES ? 0 : st + STAGE_BYTES; };
-    auto next = [&](At &a) __attribute__((always_inline)) {
-        if (++a.tile == y_tiles) {
-            a.tile = t0;
-            ++a.head;
-        }
-        a.stage = next_stage(a.stage);
+    const unsigned char *g1, *g2, *gs = nullptr;
+    auto find_tiles = [&]() __attribute__((always_inline)) {
+        const size_t at = ((size_t)((size_t)b * y_rows + (size_t)req.tile * BT) * y_heads + y_head0 + req.head) * ROW_BYTES;
+        g1 = uniform_ptr((const unsigned char *)(KEYS ? p.q : p.k) + at);
+        g2 = uniform_ptr((const unsigned char *)(KEYS ? p.dout : p.v) + at);
+        if (KEYS) gs = uniform_ptr((const unsigned char *)(p.stats + ((size_t)((size_t)b * p.Hq + y_head0 + req.head) * p.qtiles + req.tile) * (2 * BT)));
     };
+    find_tiles();
     constexpr int PER_STEP = KEYS ? 5 : 4;
-    int row_off[2];                                 // this lane's place in a whole tile
+    // this lane's place in a tile, and in the last one, where rows past the end read its last row again
+    uint32_t row_off[2], row_off_last[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int row = (wave * 2 + i) * 4 + ld_r;
         row_off[i] = row * y_stride + ((ld_u ^ swz(row)) << 4);
+        row_off_last[i] = min(row, y_rows - 1 - (y_tiles - 1) * BT) * y_stride + ((ld_u ^ swz(row)) << 4);
     }
     // part n of the requests for a step
     auto request_part = [&](int n) __attribute__((always_inline)) {
+        const uint32_t to = lds0 + req.stage;
         if (n < 4) {
             const int i = n & 1;
-            const size_t at = ((size_t)((size_t)b * y_rows + (size_t)req.tile * BT) * y_heads + y_head0 + req.head) * ROW_BYTES;
-            uint32_t o = row_off[i];
-            const int last = y_rows - 1 - req.tile * BT;
-            if (last < BT - 1) {                    // rows past the end read the last one again
-                const int row = (wave * 2 + i) * 4 + ld_r;
-                o = (uint32_t)min(row, last) * y_stride + ((ld_u ^ swz(row)) << 4);
-            }
-            lds_dma16(uniform_ptr((n < 2 ? y1 : y2) + at), o,
-                      __builtin_amdgcn_readfirstlane(lds0 + req.stage + wave * 2048 + (n < 2 ? 0 : TILE_BYTES) + i * 1024));
+            lds_dma16(n < 2 ? g1 : g2, req.tile == y_tiles - 1 ? row_off_last[i] : row_off[i],
+                      __builtin_amdgcn_readfirstlane(to + wave * 2048 + (n < 2 ? 0 : TILE_BYTES) + i * 1024));
         } else {
-            const float *st = p.stats + ((size_t)((size_t)b * p.Hq + y_head0 + req.head) * p.qtiles + req.tile) * (2 * BT);
-            lds_dma4(uniform_ptr((const unsigned char *)st), lane * 4,
-                     __builtin_amdgcn_readfirstlane(lds0 + req.stage + 2 * TILE_BYTES + wave * STATS_BYTES));
+            lds_dma4(gs, lane * 4, __builtin_amdgcn_readfirstlane(to + 2 * TILE_BYTES + wave * STATS_BYTES));
         }
     };
     // past the end the last step's tiles are read again, into stages that nobody reads, so that the number in flight stays the same
     int left = steps;
     auto request_done = [&]() __attribute__((always_inline)) {
-        const At was = req;
-        next(req);
-        if (--left <= 0) {
-            req.tile = was.tile;
-            req.head = was.head;
+        req.stage = next_stage(req.stage);
+        if (--left <= 0) return;
+        if (KEYS && req.tile == y_tiles - 1) {
+            req.tile = t0;
+            ++req.head;
+            find_tiles();
+        } else {
+            ++req.tile;
+            g1 += BT * (size_t)y_stride;
+            g2 += BT * (size_t)y_stride;
+            if (KEYS) gs += 2 * BT * sizeof(float);
         }
     };
 
@@ -289,16 +302,16 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
     float nl[NT];
     const LDS_AS unsigned char *x2l = lds + X2_BASE + wave * (NT * 32 * ROW_BYTES);
     {
-        const __bf16 *g1 = KEYS ? p.k : p.q, *g2 = KEYS ? p.v : p.dout;
+        const __bf16 *xg1 = KEYS ? p.k : p.q, *xg2 = KEYS ? p.v : p.dout;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int row = min(x0 + 32 * t + l32, x_rows - 1);
             const size_t at = ((size_t)((size_t)b * x_rows + row) * x_heads + x_head) * HD + 8 * hh;
 #pragma unroll
-            for (int s = 0; s < 8; ++s) x1[t][s] = *(const bf16x8 *)(g1 + at + 16 * s);
+            for (int s = 0; s < 8; ++s) x1[t][s] = *(const bf16x8 *)(xg1 + at + 16 * s);
             if (!KEYS) {
 #pragma unroll
-                for (int s = 0; s < 8; ++s) x2[t][s] = *(const bf16x8 *)(g2 + at + 16 * s);
+                for (int s = 0; s < 8; ++s) x2[t][s] = *(const bf16x8 *)(xg2 + at + 16 * s);
                 const int i = min(x0 + 32 * t + l32, p.Sq - 1);
                 const float *st = p.stats + ((size_t)((size_t)b * p.Hq + x_head) * p.qtiles + (i >> 5)) * (2 * BT) + (i & 31);
                 nl[t] = st[0];
@@ -309,7 +322,7 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
         }
         if (KEYS) {             // (V in registers as well: no room beside K, two accumulators of its size and the scores)
             const int first = min(x0, x_rows - 1), last = x_rows - 1 - first;
-            const unsigned char *g = uniform_ptr((const unsigned char *)(g2 + ((size_t)((size_t)b * x_rows + first) * x_heads + x_head) * HD));
+            const unsigned char *g = uniform_ptr((const unsigned char *)(xg2 + ((size_t)((size_t)b * x_rows + first) * x_heads + x_head) * HD));
 #pragma unroll
             for (int i = 0; i < 8 * NT; ++i) {
                 const int row = 4 * i + ld_r;
@@ -484,7 +497,9 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
         });
         mask([&](int t, int r, bool ok) __attribute__((always_inline)) { dp[t][r] = ok ? dp[t][r] : 0.0f; });
         stage1 = cur.stage;
-        next(cur);
+        cur.stage = next_stage(cur.stage);
+        if (KEYS && cur.tile == y_tiles - 1) cur.tile = t0;
+        else ++cur.tile;
     };
     if (steps > 0) {
 #pragma unroll
@@ -493,7 +508,8 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
             for (int n = 0; n < PER_STEP; ++n) request_part(n);
             request_done();
         }
-        __builtin_amdgcn_s_waitcnt(wait_vmcnt(PER_STEP));
+        // (all of them, so that the compiler, which counts the loads above but not these, has none left to wait for in the loop)
+        __builtin_amdgcn_s_waitcnt(0);
         wg_barrier();
 #pragma unroll
         for (int f = 0; f < LEAD; ++f) fetch(f, 0, 0, 0);
@@ -520,14 +536,13 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
             if (KEYS) acc_ready(acc2[t][d]);
         }
     // ---- results: lane = held row, registers 4 d's; exchanged with lane ^ 32, eight in line
-    const int splits = KEYS ? p.keys.splits : p.rows.splits;
     auto store = [&](f32x16 (&acc)[NT][4], float f, __bf16 *out, float *part) __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int row = x0 + 32 * t + l32;
             const bool valid = row < x_rows;
             const size_t at = ((size_t)((size_t)b * x_rows + (valid ? row : 0)) * x_heads + x_head) * HD;
-            if (splits == 1) {
+            if (n_pieces == 1) {
                 unsigned char *op = (unsigned char *)(out + at + 8 * hh);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -553,52 +568,90 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int s
     };
     const size_t all = (size_t)p.B * x_rows * x_heads * HD;
     if (KEYS) {
-        store(acc1, p.scale, p.dk, p.part_kv + (size_t)split * 2 * all);
-        store(acc2, 1.0f, p.dv, p.part_kv + ((size_t)split * 2 + 1) * all);
+        store(acc1, p.scale, p.dk, p.part_kv + (size_t)piece * 2 * all);
+        store(acc2, 1.0f, p.dv, p.part_kv + ((size_t)piece * 2 + 1) * all);
     } else {
-        store(acc1, p.scale, p.dq, p.part_q + (size_t)split * all);
+        store(acc1, p.scale, p.dq, p.part_q + (size_t)piece * all);
     }
+}
+
+// Which item the n-th workgroup of a kind takes: longest tiles first.  The hardware deals workgroups round-robin to the 8 XCDs, each with an L2 of its own;
+// where the groups (batch entries x K/V heads) divide among them, an XCD keeps to its own groups, a window of them at a time, so that
+// the tiles of a group, which stream the same data, meet in one L2.
+__device__ __forceinline__ void find_item(const Role &r, int n, int &group, int &tile, int &piece)
+{
+    int width = r.groups, base = 0, at = n;
+    if (r.window) {
+        const int per_xcd = r.groups >> 3, per_window = r.window * r.tiles * r.splits;
+        at = n >> 3;
+        const int w = at / per_window;
+        at -= w * per_window;
+        width = min(r.window, per_xcd - w * r.window);
+        base = (n & 7) * per_xcd + w * r.window;
+    }
+    const int per_tile = width * r.splits;
+    tile = at / per_tile;
+    at -= tile * per_tile;
+    piece = at / width;
+    group = base + at - piece * width;
 }
 
 template <int NT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3 - NT, 3 - NT))) void attn_bwd_kernel(const Params p)
 {
-    int n = blockIdx.x;
-    if (n < p.rows.first) {
-        const int per = p.keys.groups * p.keys.splits;
-        const int tile = n / per;
-        n -= tile * per;
-        const int split = n / p.keys.groups;
-        item<true, NT>(p, n - split * p.keys.groups, tile, split);
+    const int n = blockIdx.x;
+    int group, tile, piece;
+    if (n < p.keys.items) {
+        find_item(p.keys, n, group, tile, piece);
+        item<true, NT>(p, group, tile, piece);
     } else {
-        n -= p.rows.first;
-        const int per = p.rows.groups * p.rows.splits;
-        const int tile = n / per;
-        n -= tile * per;
-        const int split = n / p.rows.groups;
-        item<false, NT>(p, n - split * p.rows.groups, p.rows.tiles - 1 - tile, split);
+        find_item(p.rows, n - p.keys.items, group, tile, piece);
+        item<false, NT>(p, group, p.rows.tiles - 1 - tile, piece);
     }
 }
 
-// Sum of the parts of an output, in the order of the parts.
-__global__ __launch_bounds__(256) void attn_bwd_join(const float *part, __bf16 *out, size_t n8, size_t stride, int splits)
+// The sum of the parts of each tile that was cut, in the order of its pieces: 8 elements per thread, first those of dk and dv, then of dq.
+template <int NT>
+__global__ __launch_bounds__(256) void attn_bwd_join(const Params p, uint32_t kv_blocks)
 {
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n8) return;
-    f32x4 a = {0, 0, 0, 0}, c = {0, 0, 0, 0};
-    for (int s = 0; s < splits; ++s) {
-        const f32x4 *at = (const f32x4 *)(part + (size_t)s * stride) + 2 * i;
-        a += at[0];
-        c += at[1];
+    const bool keys = blockIdx.x < kv_blocks;
+    const int S = keys ? p.Skv : p.Sq, H = keys ? p.Hkv : p.Hq;
+    const size_t all = (size_t)p.B * S * H * HD;
+    const size_t i = ((size_t)(blockIdx.x - (keys ? 0 : kv_blocks)) * 256 + threadIdx.x) * 8;
+    if (i >= all) return;
+    const int pos = (int)((i / HD / H) % S);
+    int n;
+    if (keys) {
+        const int tile = pos / (128 * NT);
+        n = pieces((p.qtiles - keys_skip(p, tile, NT)) * p.G, p.keys.most);
+    } else {
+        const int tile = pos / (128 * NT / p.pack);
+        n = pieces(rows_steps(p, tile, NT), p.rows.most);
     }
-    const u32x4 w = {pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(c[0], c[1]), pack_bf16(c[2], c[3])};
-    *((u32x4 *)out + i) = w;
+    if (n == 1) return;
+    auto sum = [&](const float *part, size_t stride, __bf16 *out) {
+        f32x4 a = {0, 0, 0, 0}, c = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int s = 0; s < n; ++s) {
+            const f32x4 *at = (const f32x4 *)(part + (size_t)s * stride + i);
+            a += at[0];
+            c += at[1];
+        }
+        const u32x4 w = {pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(c[0], c[1]), pack_bf16(c[2], c[3])};
+        *(u32x4 *)(out + i) = w;
+    };
+    if (keys) {
+        sum(p.part_kv, 2 * all, p.dk);
+        sum(p.part_kv + all, 2 * all, p.dv);
+    } else {
+        sum(p.part_q, all, p.dq);
+    }
 }
 
 // ----------------------------------------------------------------------------------------------------------- host
 struct Plan {
-    int nt, pack, chunks, qtiles;
-    Role keys, rows;
+    int nt;
+    Params p;                                   // sizes and roles
     size_t stats, part_kv, part_q, total;       // bytes: the workspace's three parts
 };
 
@@ -611,24 +664,88 @@ int check_sizes(int B, int Hq, int Hkv, int Sq, int Skv, int D)
     return ATTN_OK;
 }
 
+constexpr int CUS = 256;        // of the device that this is written for: how items are cut (and so what the workspace needs) does not ask the device
+
+// How tiles are cut.  One workgroup is resident per compute unit.  Microseconds: what a step takes and what an item takes beside its steps.
+constexpr double KEYS_STEP = 1.6, ROWS_STEP = 1.25, ITEM = 7.0, JOIN = 4.0, JOIN_BYTES = 4.0e6;
+
+void deal(Role &r)
+{
+    r.items = r.groups * r.tiles * r.splits;
+    r.window = 0;
+    if (r.groups % 8 == 0) {
+        // all groups of an XCD at once, longest tiles first, while that is few rounds; then as many as occupy its 32 compute units
+        const int per_xcd = r.groups / 8, per_group = r.tiles * r.splits;
+        r.window = per_xcd * per_group <= 4 * CUS / 8 ? per_xcd : (CUS / 8 + per_group - 1) / per_group;
+    }
+}
+
 int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &r)
 {
+    Params &p = r.p;
     const int G = Hq / Hkv;
-    r.pack = G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1;
-    r.chunks = G / r.pack;
-    r.qtiles = (Sq + BT - 1) / BT;
-    r.nt = 2;
-    const int pos = 128 * r.nt / r.pack, keys = 128 * r.nt;
-    r.keys = {B * Hkv, (Skv + keys - 1) / keys, 1, 0};
-    r.rows = {B * Hkv * r.chunks, (Sq + pos - 1) / pos, 1, 0};
-    const long long nk = (long long)r.keys.groups * r.keys.tiles * r.keys.splits, nr = (long long)r.rows.groups * r.rows.tiles * r.rows.splits;
-    r.rows.first = (int)nk;
-    if ((long long)B * Hkv * r.chunks >= (1ll << 24) || nk + nr >= (1ll << 24) || B > 65535 || (long long)r.qtiles * BT * Hq >= (1ll << 32) - 64)
+    p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.Sq = Sq; p.Skv = Skv; p.G = G;
+    p.pack = G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1;
+    p.chunks = G / p.pack;
+    p.qtiles = (Sq + BT - 1) / BT;
+    // (i + INT32_MAX - Sq - 256 is above every key for i >= 0 and within 32 bits for the i < Sq + 256 of a tile)
+    p.off = causal ? Skv - Sq : INT32_MAX - Sq - 256;
+    const int nt = r.nt = 2;
+    const int pos = 128 * nt / p.pack, keys = 128 * nt;
+    const long long nk = (long long)B * Hkv * ((Skv + keys - 1) / keys), nr = (long long)B * Hkv * p.chunks * ((Sq + pos - 1) / pos);
+    if (nk >= (1ll << 23) || nr >= (1ll << 23) || B > 65535 || (long long)p.qtiles * BT * Hq >= (1ll << 32) - 64 ||
+        (long long)p.qtiles * G >= (1ll << 31))
         return ATTN_E_UNSUPPORTED;
+    p.keys = {B * Hkv, (Skv + keys - 1) / keys, 1, INT32_MAX, 0, 0};
+    p.rows = {B * Hkv * p.chunks, (Sq + pos - 1) / pos, 1, INT32_MAX, 0, 0};
+
+    // The longest tiles and the steps of all; the calls that are worth cutting are few tiles for the chip.
+    const int long_k = (p.qtiles - keys_skip(p, 0, nt)) * G, long_r = rows_steps(p, p.rows.tiles - 1, nt);
+    if (nk + nr < 8 * CUS) {
+        double all_k = 0, all_r = 0;
+        for (int t = 0; t < p.keys.tiles; ++t) all_k += (p.qtiles - keys_skip(p, t, nt)) * G;
+        for (int t = 0; t < p.rows.tiles; ++t) all_r += rows_steps(p, t, nt);
+        all_k *= p.keys.groups;
+        all_r *= p.rows.groups;
+        const double kv_bytes = 2.0 * B * Skv * Hkv * HD * 4, q_bytes = (double)B * Sq * Hq * HD * 4;
+        double best = INFINITY;
+        int best_k = 1, best_r = 1;
+        for (int sk = 1; sk <= 32; sk += sk < 8 ? 1 : sk / 4) {
+            const int mk = (long_k + sk - 1) / sk;
+            if (sk > 1 && mk < 3) break;
+            for (int sr = 1; sr <= 32; sr += sr < 8 ? 1 : sr / 4) {
+                const int mr = (long_r + sr - 1) / sr;
+                if (sr > 1 && mr < 4) break;
+                // pieces, about: a tile has steps / most of them and half of one more, if it is cut
+                const double pk = nk + (sk > 1 ? all_k / mk - 0.5 * nk : 0), pr = nr + (sr > 1 ? all_r / mr - 0.5 * nr : 0);
+                const double ik = ITEM + KEYS_STEP * mk, ir = ITEM + ROWS_STEP * mr;
+                const double work = (all_k * KEYS_STEP + all_r * ROWS_STEP + (pk + pr) * ITEM) / CUS;
+                double us = work + 0.5 * (pk + pr > CUS ? ir : 0);
+                if (us < ik) us = ik;
+                if (us < ir) us = ir;
+                if (sk > 1 || sr > 1) us += JOIN + 2 * ((sk > 1 ? sk * kv_bytes : 0) + (sr > 1 ? sr * q_bytes : 0)) / JOIN_BYTES;
+                if (us < best) {
+                    best = us;
+                    best_k = sk;
+                    best_r = sr;
+                }
+            }
+        }
+        if (best_k > 1) {
+            p.keys.most = (long_k + best_k - 1) / best_k;
+            p.keys.splits = pieces(long_k, p.keys.most);
+        }
+        if (best_r > 1) {
+            p.rows.most = (long_r + best_r - 1) / best_r;
+            p.rows.splits = pieces(long_r, p.rows.most);
+        }
+    }
+    deal(p.keys);
+    deal(p.rows);
     auto pad = [](size_t n) { return (n + 255) / 256 * 256; };
-    r.stats = pad((size_t)B * Hq * r.qtiles * 2 * BT * sizeof(float));
-    r.part_kv = r.keys.splits > 1 ? pad((size_t)r.keys.splits * 2 * B * Skv * Hkv * HD * sizeof(float)) : 0;
-    r.part_q = r.rows.splits > 1 ? pad((size_t)r.rows.splits * B * Sq * Hq * HD * sizeof(float)) : 0;
+    r.stats = pad((size_t)B * Hq * p.qtiles * 2 * BT * sizeof(float));
+    r.part_kv = p.keys.splits > 1 ? pad((size_t)p.keys.splits * 2 * B * Skv * Hkv * HD * sizeof(float)) : 0;
+    r.part_q = p.rows.splits > 1 ? pad((size_t)p.rows.splits * B * Sq * Hq * HD * sizeof(float)) : 0;
     r.total = r.stats + r.part_kv + r.part_q;
     return ATTN_OK;
 }
@@ -680,40 +797,32 @@ int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, 
     }
     hipStream_t st = (hipStream_t)stream;
 
-    Params p = {};
+    Params &p = r.p;
     p.q = (const __bf16 *)q; p.k = (const __bf16 *)k; p.v = (const __bf16 *)v; p.dout = (const __bf16 *)dout;
     p.dq = (__bf16 *)dq; p.dk = (__bf16 *)dk; p.dv = (__bf16 *)dv;
     p.stats = (const float *)workspace;
     p.part_kv = (float *)((unsigned char *)workspace + r.stats);
     p.part_q = (float *)((unsigned char *)workspace + r.stats + r.part_kv);
-    p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.Sq = Sq; p.Skv = Skv; p.G = Hq / Hkv; p.qtiles = r.qtiles;
-    p.pack = r.pack; p.chunks = r.chunks;
-    // (i + INT32_MAX - Sq - 256 is above every key for i >= 0 and within 32 bits for the i < Sq + 256 of a tile)
-    p.off = causal ? Skv - Sq : INT32_MAX - Sq - 256;
     p.c = scale * LOG2E;
     p.scale = scale;
-    p.keys = r.keys; p.rows = r.rows;
 
     {
         float *stats = (float *)workspace;
-        unsigned rows = (unsigned)r.qtiles * BT * (unsigned)Hq;
-        void *args[] = {(void *)&dout, (void *)&o, (void *)&lse, (void *)&dlse, &stats, &Hq, &Sq, &r.qtiles, &rows};
+        unsigned rows = (unsigned)p.qtiles * BT * (unsigned)Hq;
+        void *args[] = {(void *)&dout, (void *)&o, (void *)&lse, (void *)&dlse, &stats, &Hq, &Sq, &p.qtiles, &rows};
         if (!launch((const void *)attn_bwd_stats, dim3((rows + 63) / 64, B), 256, 0, args, st)) return ATTN_E_LAUNCH;
     }
     {
         void *args[] = {&p};
-        const int items = r.rows.first + r.rows.groups * r.rows.tiles * r.rows.splits;
-        if (!launch((const void *)attn_bwd_kernel<2>, dim3(items), 256, lds_bytes(2), args, st)) return ATTN_E_LAUNCH;
+        if (!launch((const void *)attn_bwd_kernel<2>, dim3(p.keys.items + p.rows.items), 256, lds_bytes(2), args, st)) return ATTN_E_LAUNCH;
     }
-    auto join = [&](const float *part, void *out, size_t n, size_t stride, int splits) -> bool {
-        size_t n8 = n / 8;
-        void *args[] = {&part, &out, &n8, &stride, &splits};
-        return launch((const void *)attn_bwd_join, dim3((unsigned)((n8 + 255) / 256)), 256, 0, args, st);
-    };
-    const size_t nq = (size_t)B * Sq * Hq * HD, nkv = (size_t)B * Skv * Hkv * HD;
-    if (r.keys.splits > 1 && !(join(p.part_kv, dk, nkv, 2 * nkv, r.keys.splits) && join(p.part_kv + nkv, dv, nkv, 2 * nkv, r.keys.splits)))
-        return ATTN_E_LAUNCH;
-    if (r.rows.splits > 1 && !join(p.part_q, dq, nq, nq, r.rows.splits)) return ATTN_E_LAUNCH;
+    if (p.keys.splits > 1 || p.rows.splits > 1) {
+        auto blocks = [](size_t n) { return (uint32_t)((n / 8 + 255) / 256); };
+        uint32_t kv_blocks = p.keys.splits > 1 ? blocks((size_t)B * Skv * Hkv * HD) : 0;
+        const uint32_t q_blocks = p.rows.splits > 1 ? blocks((size_t)B * Sq * Hq * HD) : 0;
+        void *args[] = {&p, &kv_blocks};
+        if (!launch((const void *)attn_bwd_join<2>, dim3(kv_blocks + q_blocks), 256, 0, args, st)) return ATTN_E_LAUNCH;
+    }
     return ATTN_OK;
 }
 
