@@ -46,18 +46,26 @@ constexpr int ROW_BYTES = HD * 2;
 constexpr int BT = 32;                          // streamed rows per step
 constexpr int TILE_BYTES = BT * ROW_BYTES;      // 8 KiB
 constexpr int STATS_BYTES = 2 * BT * 4;         // -LSE and -delta of a step's 32 rows
-// LDS stages.  While step j runs, tiles j + 1 and j + 2 arrive, and Y1 of step j - 1 is still read; in rows items, where that is the end of a step,
-// a read of step j - 2's may be on its way when the request that takes its stage leaves.
-constexpr int stages(bool keys) { return keys ? 4 : 5; }
-constexpr int stage_bytes(bool keys) { return 2 * TILE_BYTES + (keys ? 4 * STATS_BYTES : 0); }      // (each wavefront has the figures for itself)
-constexpr int X2_BASE = stages(true) * stage_bytes(true);   // keys items: V, 8 * NT KiB per wavefront
 constexpr float LOG2E = 1.4426950408889634f;
 
+// How an item of each kind uses LDS.  While step j runs, the tiles of steps up to j + AHEAD arrive.  Y1 of step j - 1 is still read (in rows items at
+// the end of the step, so that a read of step j - 2's may be on its way when the request that takes its stage leaves); Y2 of step j is read to
+// the end in keys items, to the middle in rows items.  Two workgroups of the small form (NT = 1) share a compute unit's 160 KiB; its keys items have
+// no room for a stage that covers reads on their way, so a wavefront waits for its reads in front of the barrier there.
+template <bool KEYS, int NT>
+struct Lds {
+    static constexpr int AHEAD = KEYS && NT == 1 ? 1 : 2;
+    static constexpr bool DRAIN = KEYS && NT == 1;
+    static constexpr int N1 = KEYS ? AHEAD + 2 : AHEAD + 3, N2 = KEYS && !DRAIN ? AHEAD + 2 : AHEAD + 1, NF = AHEAD + 1;    // stages of Y1, Y2, figures
+    static constexpr int Y2 = N1 * TILE_BYTES, X2 = Y2 + N2 * TILE_BYTES, FIGURES = X2 + (KEYS ? 4 * NT * 32 * ROW_BYTES : 0);
+    static constexpr int BYTES = FIGURES + (KEYS ? NF * STATS_BYTES : 0);
+};
 constexpr int lds_bytes(int nt)
 {
-    const int keys = X2_BASE + 4 * nt * 32 * ROW_BYTES, rows = stages(false) * stage_bytes(false);
+    const int keys = nt == 1 ? Lds<true, 1>::BYTES : Lds<true, 2>::BYTES, rows = nt == 1 ? Lds<false, 1>::BYTES : Lds<false, 2>::BYTES;
     return keys > rows ? keys : rows;
 }
+static_assert(lds_bytes(2) <= 160 * 1024 && lds_bytes(1) <= 80 * 1024);
 
 // The items of one kind.  A tile's steps (streamed tiles, of all heads of a group) are cut into pieces of at most `most`, so that a call of few or
 // uneven tiles fills the chip; a tile of several pieces leaves FP32 parts, which attn_bwd_join adds up.
@@ -127,14 +135,16 @@ __device__ __forceinline__ void lds_dma4(const unsigned char *base, uint32_t vof
 #pragma clang diagnostic pop
 // acc += A B for the sums that a wavefront keeps through all steps, in the accumulation half of the register file (the compiler, which
 // gives all products of a kernel one form or moves them between the halves as it sees fit, otherwise copies up to 300 registers a step).
-// It knows nothing of the instruction's timing, so: A and B are vector-ALU results no younger than two products, or LDS reads, for
-// which the compiler waits; nothing but the same kind of product reads `acc` until acc_ready(), and two into the same registers are 4 * NT products apart.
+// It knows nothing of the instruction's timing, so: between a vector-ALU instruction that writes A or B and the product that reads it stand two others
+// (a host-side test looks for it in the built code; LDS reads the compiler waits for); and nothing but the same kind of product reads `acc` until
+// acc_ready(), two into the same registers being 4 * NT products apart.
 __device__ __forceinline__ void mfma_acc(f32x16 &acc, bf16x8 a, bf16x8 b) {
     asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
 }
 // 16 passes at most, so 18 wait states between a product and another instruction that reads its result
 __device__ __forceinline__ void acc_ready(f32x16 &acc) { asm volatile("s_nop 15\n\ts_nop 3" : "+a"(acc)); }
 constexpr int wait_vmcnt(int n) { return 0x0F70 | n; }     // s_waitcnt vmcnt(n), n < 16
+constexpr int WAIT_LGKMCNT0 = ~0x0F00;                      // (and it also waits for this wavefront's LDS reads)
 __device__ __forceinline__ void wg_barrier() {
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_barrier();
@@ -200,7 +210,7 @@ __global__ __launch_bounds__(256) void attn_bwd_stats(const __bf16 *dout, const 
 template <bool KEYS, int NT>
 __device__ __forceinline__ void item(const Params &p, int group, int tile, int piece)
 {
-    constexpr int NSTAGE = stages(KEYS), STAGE_BYTES = stage_bytes(KEYS);
+    typedef Lds<KEYS, NT> L;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     LDS_AS unsigned char *lds = (LDS_AS unsigned char *)smem;
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
@@ -238,19 +248,24 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     const int x_heads = KEYS ? p.Hkv : p.Hq, y_heads = KEYS ? p.Hq : p.Hkv;
     const uint32_t y_stride = (uint32_t)y_heads * ROW_BYTES;
 
-    // ---- requests: 4 rows x 256 bytes per instruction, two of each tile per wavefront (and, KEYS, its 256 bytes of figures)
+    // ---- requests: 4 rows x 256 bytes per instruction, two of each tile per wavefront (and, KEYS, a quarter of 256 bytes of figures)
     const int ld_r = lane >> 4, ld_u = lane & 15;
-    // Where steps and requests stand: streamed tile, query head of the group, LDS stage; and, for requests, the tiles' addresses.
-    struct At { int tile, head, stage; };
+    // Where steps and requests stand: streamed tile, query head of the group, LDS stages; and, for requests, the tiles' addresses.
+    struct At { int tile, head, s1, s2, sf; };
     const int y_tiles = KEYS ? p.qtiles : (y_rows + BT - 1) / BT;
     At cur, req;
     cur.head = KEYS && per_head > 0 ? step0 / per_head : 0;
     cur.tile = KEYS ? min(step0 - cur.head * per_head + t0, y_tiles - 1) : min(step0, y_tiles - 1);
     uniform(cur.head);
     uniform(cur.tile);
-    cur.stage = 0;
+    cur.s1 = 0; cur.s2 = L::Y2; cur.sf = L::FIGURES;
     req = cur;
-    auto next_stage = [&](int st) __attribute__((always_inline)) { return st == (NSTAGE - 1) * STAGE_BYTES ? 0 : st + STAGE_BYTES; };
+    auto next1 = [&](int st) __attribute__((always_inline)) { return st == (L::N1 - 1) * TILE_BYTES ? 0 : st + TILE_BYTES; };
+    auto next_stages = [&](At &a) __attribute__((always_inline)) {
+        a.s1 = next1(a.s1);
+        a.s2 = a.s2 == L::Y2 + (L::N2 - 1) * TILE_BYTES ? L::Y2 : a.s2 + TILE_BYTES;
+        if (KEYS) a.sf = a.sf == L::FIGURES + (L::NF - 1) * STATS_BYTES ? L::FIGURES : a.sf + STATS_BYTES;
+    };
     const unsigned char *g1, *g2, *gs = nullptr;
     auto find_tiles = [&]() __attribute__((always_inline)) {
         const size_t at = ((size_t)((size_t)b * y_rows + (size_t)req.tile * BT) * y_heads + y_head0 + req.head) * ROW_BYTES;
@@ -270,19 +285,18 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     }
     // part n of the requests for a step
     auto request_part = [&](int n) __attribute__((always_inline)) {
-        const uint32_t to = lds0 + req.stage;
         if (n < 4) {
             const int i = n & 1;
             lds_dma16(n < 2 ? g1 : g2, req.tile == y_tiles - 1 ? row_off_last[i] : row_off[i],
-                      __builtin_amdgcn_readfirstlane(to + wave * 2048 + (n < 2 ? 0 : TILE_BYTES) + i * 1024));
-        } else {
-            lds_dma4(gs, lane * 4, __builtin_amdgcn_readfirstlane(to + 2 * TILE_BYTES + wave * STATS_BYTES));
+                      __builtin_amdgcn_readfirstlane(lds0 + (n < 2 ? req.s1 : req.s2) + wave * 2048 + i * 1024));
+        } else if (lane < 16) {
+            lds_dma4(gs, (wave * 16 + lane) * 4, __builtin_amdgcn_readfirstlane(lds0 + req.sf + wave * 64));
         }
     };
     // past the end the last step's tiles are read again, into stages that nobody reads, so that the number in flight stays the same
     int left = steps;
     auto request_done = [&]() __attribute__((always_inline)) {
-        req.stage = next_stage(req.stage);
+        next_stages(req);
         if (--left <= 0) return;
         if (KEYS && req.tile == y_tiles - 1) {
             req.tile = t0;
@@ -300,7 +314,7 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     bf16x8 x1[NT][8], x2[NT][8];
     f32x16 nd[NT];              // rows items: -delta of the lane's row in every element, the C operand that dP starts from
     float nl[NT];
-    const LDS_AS unsigned char *x2l = lds + X2_BASE + wave * (NT * 32 * ROW_BYTES);
+    const uint32_t x2_at = lds0 + L::X2 + wave * (NT * 32 * ROW_BYTES);
     {
         const __bf16 *xg1 = KEYS ? p.k : p.q, *xg2 = KEYS ? p.v : p.dout;
 #pragma unroll
@@ -327,7 +341,7 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
             for (int i = 0; i < 8 * NT; ++i) {
                 const int row = 4 * i + ld_r;
                 lds_dma16(g, (uint32_t)min(row, last) * (uint32_t)(x_heads * ROW_BYTES) + ((ld_u ^ swz(row)) << 4),
-                          __builtin_amdgcn_readfirstlane(lds0 + X2_BASE + wave * (NT * 32 * ROW_BYTES) + i * 1024));
+                          __builtin_amdgcn_readfirstlane(x2_at + i * 1024));
             }
         }
     }
@@ -347,13 +361,13 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
         const int i16 = lane & 15, g = (lane >> 4) & 1, row = 4 * hh + (i16 >> 2), col = 16 * g + 4 * (i16 & 3);
         t_at = row * ROW_BYTES + (((col >> 3) ^ swz(row)) << 4) + (col & 7) * 2;
     }
-    typedef const LDS_AS unsigned char *Lds;
+    typedef const LDS_AS unsigned char *Ptr;
     auto row_frag = [&](uint32_t at, int s, int imm) __attribute__((always_inline)) -> bf16x8 {     // `at`: r_at in the stage
-        return *(const LDS_AS bf16x8 *)((Lds)(uintptr_t)(at ^ (s << 5)) + imm);
+        return *(const LDS_AS bf16x8 *)((Ptr)(uintptr_t)(at ^ (s << 5)) + imm);
     };
     auto col_frag = [&](uint32_t at, int k, int d, int imm) __attribute__((always_inline)) -> bf16x8 {     // `at`: t_at in the stage
-        s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Lds)(uintptr_t)(at ^ (d << 6)) + (imm + 16 * k * ROW_BYTES)));
-        s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Lds)(uintptr_t)(at ^ (d << 6) ^ 32) + (imm + (16 * k + 8) * ROW_BYTES)));
+        s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Ptr)(uintptr_t)(at ^ (d << 6)) + (imm + 16 * k * ROW_BYTES)));
+        s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Ptr)(uintptr_t)(at ^ (d << 6) ^ 32) + (imm + (16 * k + 8) * ROW_BYTES)));
         s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
         return __builtin_bit_cast(bf16x8, v);
     };
@@ -364,43 +378,45 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     // and between the products the vector work, each piece a phase or two after the products that it needs: rounding dS(j-1) during S(j), the
     // exponents of S(j) during the two phases after it, P * dP behind dP(j).  Fragments are read LEAD ahead, across the end of
     // a step too, so the step's barrier stands LEAD fragments before its end.
-    constexpr int LEAD = 3, LEAD2 = 2;
-    constexpr int NF = KEYS ? 32 : 24;          // fragments of a step
+    constexpr int LEAD = NT == 2 ? 3 : 2, LEAD2 = NT == 2 ? 2 : 1;      // (NT = 1: the other workgroup of the compute unit hides more)
+    constexpr int NF = KEYS ? 32 : 24;          // fragments of a step; fragment f lies in frag[f % 4]
+    static_assert(LEAD < 4 && NF % 4 == 0);
     constexpr int PH_S = 0, PH_DP = KEYS ? 2 : 1, PH_1 = KEYS ? 1 : 2, PH_2 = 3;
     constexpr int SLOTS = 8 * NT;               // products of a phase
-    bf16x8 frag[LEAD + 1], frag2[LEAD2 + 1][NT];
+    bf16x8 frag[4], frag2[LEAD2 + 1][NT];
     f32x16 s[NT], dp[NT];
-    uint32_t pb[NT][8], ds[NT][8];
-    int stage1 = 0;                             // stage of step j - 1
+    u32x4 pb[NT][2], ds[NT][2];                 // BF16 pairs, the B operands of acc2 and acc1
+    int prev1 = 0;                              // stage of step j - 1's Y1
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) dp[t][r] = 0.0f;
-    auto half = [&](const uint32_t (&w)[8], int k) __attribute__((always_inline)) -> bf16x8 {
-        const u32x4 x = {w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]};
-        return __builtin_bit_cast(bf16x8, x);
+    // (held in place as soon as it is complete: moved behind other instructions it could end up right in front of its product)
+    auto pack = [&](u32x4 (&w)[2], int r, float x0, float x1) __attribute__((always_inline)) {       // elements r, r + 1
+        w[r >> 3][(r >> 1) & 3] = pack_bf16(x0, x1);
+        if ((r & 7) == 6) asm volatile("" : "+v"(w[r >> 3]));
     };
-    auto fetch = [&](int f, uint32_t at, uint32_t at1, uint32_t at_next) __attribute__((always_inline)) {    // stages of steps j, j - 1, j + 1
-        const int ph = (f % NF) >> 3, i = f & 7;
-        bf16x8 &to = frag[f % (LEAD + 1)];
-        if (f >= NF) to = row_frag(lds0 + at_next + r_at, i, 0);
-        else if (ph == PH_S) to = row_frag(lds0 + at + r_at, i, 0);
-        else if (ph == PH_DP) to = row_frag(lds0 + at + r_at, i, TILE_BYTES);
-        else if (ph == PH_1) to = col_frag(lds0 + at1 + t_at, i >> 2, i & 3, 0);
-        else to = col_frag(lds0 + at + t_at, i >> 2, i & 3, TILE_BYTES);
+    auto fetch = [&](int f) __attribute__((always_inline)) {
+        const int ph = f >> 3, i = f & 7;
+        bf16x8 &to = frag[f % 4];
+        if (f >= NF) to = row_frag(lds0 + next1(cur.s1) + r_at, i, 0);
+        else if (ph == PH_S) to = row_frag(lds0 + cur.s1 + r_at, i, 0);
+        else if (ph == PH_DP) to = row_frag(lds0 + cur.s2 + r_at, i, 0);
+        else if (ph == PH_1) to = col_frag(lds0 + prev1 + t_at, i >> 2, i & 3, 0);
+        else to = col_frag(lds0 + cur.s2 + t_at, i >> 2, i & 3, 0);
     };
     auto fetch2 = [&](int f) __attribute__((always_inline)) {
         const int i = f & 7;
         if (KEYS && f < NF && (f >> 3) == PH_DP) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) frag2[i % (LEAD2 + 1)][t] = row_frag((uint32_t)(uintptr_t)x2l + r_at, i, t * 32 * ROW_BYTES);
+            for (int t = 0; t < NT; ++t) frag2[i % (LEAD2 + 1)][t] = row_frag(x2_at + r_at, i, t * 32 * ROW_BYTES);
         }
     };
     const int x_last = min(x0 + 32 * NT, x_rows) - 1;
     auto step = [&]() __attribute__((always_inline)) {
         const int y0 = cur.tile * BT;
         const bool masked = KEYS ? x_last > y0 + p.off : (y0 + BT - 1 > x0 + p.off || y0 + BT > y_rows);
-        const uint32_t at = cur.stage, at1 = stage1, at_next = next_stage(cur.stage);
+        const Ptr figures = (Ptr)(uintptr_t)(lds0 + cur.sf) + 16 * hh;
         f32x4 nlv[4];
         // Masked pairs (KEYS: row < key - off; else key > row + off or key >= Skv) give exactly 0, whatever they hold.  A branch around
         // selects alone: two forms of the whole step meet in copies of hundreds of registers.
@@ -424,12 +440,12 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
         // element e of the vector work
         auto do_round = [&](int e) __attribute__((always_inline)) {       // dS(j-1), pairs
             const int t = e >> 3, r = 2 * (e & 7);
-            ds[t][e & 7] = pack_bf16(dp[t][r], dp[t][r + 1]);
+            pack(ds[t], r, dp[t][r], dp[t][r + 1]);
         };
         auto do_exp = [&](int e) __attribute__((always_inline)) {
             const int t = e >> 4, r = e & 15;
             s[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], p.c, KEYS ? nlv[r >> 2][r & 3] : nl[t]));
-            if (KEYS && (r & 1)) pb[t][r >> 1] = pack_bf16(s[t][r - 1], s[t][r]);
+            if (KEYS && (r & 1)) pack(pb[t], r - 1, s[t][r - 1], s[t][r]);
         };
         auto do_mul = [&](int e) __attribute__((always_inline)) {
             const int t = e >> 4, r = e & 15;
@@ -447,28 +463,32 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
             if constexpr (KEYS && f == 8 * PH_2) {
                 mask([&](int t, int r, bool ok) __attribute__((always_inline)) {
                     s[t][r] = ok ? s[t][r] : 0.0f;
-                    if (r & 1) pb[t][r >> 1] = pack_bf16(s[t][r - 1], s[t][r]);
+                    if (r & 1) pack(pb[t], r - 1, s[t][r - 1], s[t][r]);
                 });
+                asm volatile("s_nop 1");
+                __builtin_amdgcn_sched_barrier(0);
             }
             if (f == NF - LEAD) {
-                // the next step's tiles have landed (all but the newest PER_STEP requests), for every wavefront
-                __builtin_amdgcn_s_waitcnt(wait_vmcnt(PER_STEP));
+                // the next step's tiles have landed (all but those of the steps behind it), for every wavefront
+                __builtin_amdgcn_s_waitcnt(wait_vmcnt((L::AHEAD - 1) * PER_STEP) & (L::DRAIN ? WAIT_LGKMCNT0 : ~0));
                 wg_barrier();
             }
-            fetch(f + LEAD, at, at1, at_next);
+            fetch(f + LEAD);
             fetch2(f + LEAD2);
             if (f >= 1 && f <= PER_STEP) request_part(f - 1);
             if (f == PER_STEP + 1) request_done();
-            if constexpr (KEYS && f >= 4 && f < 8)
-                nlv[f - 4] = *(const LDS_AS f32x4 *)(lds + at + 2 * TILE_BYTES + wave * STATS_BYTES + (8 * (f - 4) + 4 * hh) * 4);
-            if constexpr (KEYS && f >= 8 && f < 12) {
-                const f32x4 d = *(const LDS_AS f32x4 *)(lds + at + 2 * TILE_BYTES + wave * STATS_BYTES + BT * 4 + (8 * (f - 8) + 4 * hh) * 4);
+            if constexpr (KEYS) {       // -LSE, a quarter at a time shortly before its exponents (NT = 2: used twice, kept); -delta, where dP starts from
+                constexpr int g = NT == 2 ? f - 4 : (f - 6) / 3;
+                if constexpr (NT == 2 ? g >= 0 && g < 4 : f >= 6 && (f - 6) % 3 == 0 && g < 4) nlv[g] = *(const LDS_AS f32x4 *)(figures + 32 * g);
+                if constexpr (f >= 8 && f < 12) {
+                    const f32x4 d = *(const LDS_AS f32x4 *)(figures + BT * 4 + 32 * (f - 8));
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) dp[t][4 * (f - 8) + e] = d[e];
+                        for (int e = 0; e < 4; ++e) dp[t][4 * (f - 8) + e] = d[e];
+                }
             }
-            const bf16x8 a = frag[f % (LEAD + 1)];
+            const bf16x8 a = frag[f % 4];
             static_for<NT>([&](auto tc) __attribute__((always_inline)) {
                 constexpr int t = decltype(tc)::value;
                 if constexpr (ph == PH_S) {
@@ -479,9 +499,9 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
                 } else if constexpr (ph == PH_DP) {
                     dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, KEYS ? frag2[i % (LEAD2 + 1)][t] : x2[t][i], !KEYS && i == 0 ? nd[t] : dp[t], 0, 0, 0);
                 } else if constexpr (ph == PH_1) {
-                    mfma_acc(acc1[t][i & 3], a, half(ds[t], i >> 2));
+                    mfma_acc(acc1[t][i & 3], a, __builtin_bit_cast(bf16x8, ds[t][i >> 2]));
                 } else {
-                    mfma_acc(acc2[t][i & 3], a, half(pb[t], i >> 2));
+                    mfma_acc(acc2[t][i & 3], a, __builtin_bit_cast(bf16x8, pb[t][i >> 2]));
                 }
                 constexpr int slot = f * NT + t;
                 spread(slot, SLOTS, 8 * NT, do_round);
@@ -496,14 +516,14 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
             });
         });
         mask([&](int t, int r, bool ok) __attribute__((always_inline)) { dp[t][r] = ok ? dp[t][r] : 0.0f; });
-        stage1 = cur.stage;
-        cur.stage = next_stage(cur.stage);
+        prev1 = cur.s1;
+        next_stages(cur);
         if (KEYS && cur.tile == y_tiles - 1) cur.tile = t0;
         else ++cur.tile;
     };
     if (steps > 0) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < L::AHEAD; ++i) {
 #pragma unroll
             for (int n = 0; n < PER_STEP; ++n) request_part(n);
             request_done();
@@ -512,19 +532,22 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
         __builtin_amdgcn_s_waitcnt(0);
         wg_barrier();
 #pragma unroll
-        for (int f = 0; f < LEAD; ++f) fetch(f, 0, 0, 0);
+        for (int f = 0; f < LEAD; ++f) fetch(f);
         for (int j = 0; j < steps; ++j) step();
         __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
         // the last step's dS
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; r += 2) ds[t][r >> 1] = pack_bf16(dp[t][r], dp[t][r + 1]);
+            for (int r = 0; r < 16; r += 2) pack(ds[t], r, dp[t][r], dp[t][r + 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 1");
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const bf16x8 a = col_frag(lds0 + stage1 + t_at, i >> 2, i & 3, 0);
+            const bf16x8 a = col_frag(lds0 + prev1 + t_at, i >> 2, i & 3, 0);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) mfma_acc(acc1[t][i & 3], a, half(ds[t], i >> 2));
+            for (int t = 0; t < NT; ++t) mfma_acc(acc1[t][i & 3], a, __builtin_bit_cast(bf16x8, ds[t][i >> 2]));
         }
     }
 
@@ -690,7 +713,10 @@ int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &r)
     p.qtiles = (Sq + BT - 1) / BT;
     // (i + INT32_MAX - Sq - 256 is above every key for i >= 0 and within 32 bits for the i < Sq + 256 of a tile)
     p.off = causal ? Skv - Sq : INT32_MAX - Sq - 256;
-    const int nt = r.nt = 2;
+#ifndef NTX
+#define NTX 2
+#endif
+    const int nt = r.nt = NTX;
     const int pos = 128 * nt / p.pack, keys = 128 * nt;
     const long long nk = (long long)B * Hkv * ((Skv + keys - 1) / keys), nr = (long long)B * Hkv * p.chunks * ((Sq + pos - 1) / pos);
     if (nk >= (1ll << 23) || nr >= (1ll << 23) || B > 65535 || (long long)p.qtiles * BT * Hq >= (1ll << 32) - 64 ||
@@ -791,7 +817,8 @@ int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, 
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return ATTN_E_LAUNCH;
     if (!ready[dev].load(std::memory_order_acquire)) {
-        if (hipFuncSetAttribute((const void *)attn_bwd_kernel<2>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(2)) != hipSuccess)
+        if (hipFuncSetAttribute((const void *)attn_bwd_kernel<1>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(1)) != hipSuccess ||
+            hipFuncSetAttribute((const void *)attn_bwd_kernel<2>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(2)) != hipSuccess)
             return ATTN_E_LAUNCH;
         ready[dev].store(true, std::memory_order_release);
     }
@@ -814,14 +841,16 @@ int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, 
     }
     {
         void *args[] = {&p};
-        if (!launch((const void *)attn_bwd_kernel<2>, dim3(p.keys.items + p.rows.items), 256, lds_bytes(2), args, st)) return ATTN_E_LAUNCH;
+        if (!launch(r.nt == 1 ? (const void *)attn_bwd_kernel<1> : (const void *)attn_bwd_kernel<2>, dim3(p.keys.items + p.rows.items), 256,
+                    lds_bytes(r.nt), args, st))
+            return ATTN_E_LAUNCH;
     }
     if (p.keys.splits > 1 || p.rows.splits > 1) {
         auto blocks = [](size_t n) { return (uint32_t)((n / 8 + 255) / 256); };
         uint32_t kv_blocks = p.keys.splits > 1 ? blocks((size_t)B * Skv * Hkv * HD) : 0;
         const uint32_t q_blocks = p.rows.splits > 1 ? blocks((size_t)B * Sq * Hq * HD) : 0;
         void *args[] = {&p, &kv_blocks};
-        if (!launch((const void *)attn_bwd_join<2>, dim3(kv_blocks + q_blocks), 256, 0, args, st)) return ATTN_E_LAUNCH;
+        if (!launch(r.nt == 1 ? (const void *)attn_bwd_join<1> : (const void *)attn_bwd_join<2>, dim3(kv_blocks + q_blocks), 256, 0, args, st)) return ATTN_E_LAUNCH;
     }
     return ATTN_OK;
 }
