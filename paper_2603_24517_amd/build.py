@@ -30,10 +30,6 @@ HIPCC_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
 
-# Matrix products may accumulate in either half of the register file, chosen for each product, not for a whole kernel: the backward kernel
-# keeps its sums in one half and its scores, which vector instructions read, in the other.  (Without it 268 registers of that kernel spill.)
-LAYER_FLAGS = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
-
 # every launch through the 256-row kernel, in whole items: for switches that act there
 ALL_256_ROWS = ["-DATTN_SMALL_PATH=0", "-DATTN_SHARE=0"]
 # name -> extra compiler flags; what each stands for is described where the switches are defined
@@ -86,7 +82,7 @@ def build_probe(verbose=False):
 
 
 def build_layer(verbose=False):
-    return _hipcc(LAYER_FLAGS, LAYER_LIB, LAYER_SRCS, verbose)
+    return _hipcc([], LAYER_LIB, LAYER_SRCS, verbose)
 
 
 def build_call(verbose=False):

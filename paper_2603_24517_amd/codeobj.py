@@ -1,5 +1,5 @@
-"""Reads the gfx950 code objects inside a library built here: the metadata notes (register counts, scratch size, spills per
-kernel) and the instructions, for checks of waits that the compiler does not make."""
+"""Reads the metadata notes of the gfx950 code object inside a built library (register counts, scratch
+size, spills per kernel).  Metadata only: nothing is disassembled."""
 import os
 import re
 import subprocess
@@ -18,9 +18,9 @@ def _bundles(fatbin):
     return [fatbin[a:b] for a, b in zip(starts, starts[1:] + [len(fatbin)])]
 
 
-def _read(lib_path, *tool):
-    """What an LLVM tool prints for every gfx950 code object of the library."""
-    text = ""
+def kernel_metadata(lib_path):
+    """{kernel symbol: {field: int}} for every kernel of the library's gfx950 code objects."""
+    notes = ""
     with tempfile.TemporaryDirectory() as tmp:
         fatbin, part, code = (os.path.join(tmp, n) for n in ("fatbin", "part", "code.o"))
         subprocess.run([os.path.join(LLVM_BIN, "llvm-objcopy"), "-O", "binary", "--only-section=.hip_fatbin",
@@ -32,23 +32,8 @@ def _read(lib_path, *tool):
                 f.write(bundle)
             subprocess.run([os.path.join(LLVM_BIN, "clang-offload-bundler"), "--unbundle", "--type=o",
                             f"--targets={TARGET}", f"--input={part}", f"--output={code}"], check=True)
-            text += subprocess.run([os.path.join(LLVM_BIN, tool[0]), *tool[1:], code], check=True, capture_output=True, text=True).stdout
-    return text
-
-
-def disassembly(lib_path):
-    """The instructions of every kernel of the library, in order, one "name operands" each."""
-    lines = []
-    for line in _read(lib_path, "llvm-objdump", "-d", "--no-show-raw-insn").splitlines():
-        text = line.split("//")[0].split(";")[0].strip()
-        if line[:1].isspace() and text:
-            lines.append(" ".join(text.split()))
-    return lines
-
-
-def kernel_metadata(lib_path):
-    """{kernel symbol: {field: int}} for every kernel of the library's gfx950 code objects."""
-    notes = _read(lib_path, "llvm-readelf", "--notes")
+            notes += subprocess.run([os.path.join(LLVM_BIN, "llvm-readelf"), "--notes", code], check=True,
+                                    capture_output=True, text=True).stdout
     kernels = {}
     for entry in re.split(r"\n\s*- \.", notes):
         name = re.search(r"\.name:\s+(\S+)", entry)

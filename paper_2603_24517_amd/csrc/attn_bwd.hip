@@ -10,8 +10,8 @@
 // workgroups (atomics: another order, other bits, every launch, and 16 KiB of FP32 through the caches for 32 rows).
 // Here a work item holds one side in registers and streams the other, and the scores are formed in both kinds of items: seven products
 // instead of five, but no memory traffic beside inputs and outputs, and the same bits always.
-//   * a "keys" item holds K and V of 128 * NT keys and streams Q and dO of every query head that shares them;
-//   * a "rows" item holds Q and dO of 128 * NT query rows and streams K and V.
+//   * a "keys" item holds K and V of 128 keys and streams Q and dO of every query head that shares them;
+//   * a "rows" item holds Q and dO of 128 query rows and streams K and V.
 // Both are the same loop with the operands' names exchanged.  X1, X2 stand for what is held, Y1, Y2 for what streams:
 //     S = Y1 X1^T     dP = Y2 X2^T - delta     acc1 += Y1^T dS     (keys only) acc2 += Y2^T P
 // With v_mfma_f32_32x32x16_bf16 and Y as the A operand, the accumulator layout puts one held row (lane % 32) in each lane
@@ -45,35 +45,44 @@ constexpr int HD = 128;
 constexpr int ROW_BYTES = HD * 2;
 constexpr int BT = 32;                          // streamed rows per step
 constexpr int TILE_BYTES = BT * ROW_BYTES;      // 8 KiB
+constexpr int ITEM_ROWS = 128;                  // held rows of an item, 32 per wavefront
 constexpr int STATS_BYTES = 2 * BT * 4;         // -LSE and -delta of a step's 32 rows
 constexpr float LOG2E = 1.4426950408889634f;
 
 // How an item of each kind uses LDS.  While step j runs, the tiles of steps up to j + AHEAD arrive.  Y1 of step j - 1 is still read (in rows items at
 // the end of the step, so that a read of step j - 2's may be on its way when the request that takes its stage leaves); Y2 of step j is read to
-// the end in keys items, to the middle in rows items.  Two workgroups of the small form (NT = 1) share a compute unit's 160 KiB; its keys items have
-// no room for a stage that covers reads on their way, so a wavefront waits for its reads in front of the barrier there.
-template <bool KEYS, int NT>
+// the end in keys items, to the middle in rows items.  Two workgroups share a compute unit's 160 KiB; keys items, which hold V there, have
+// no room for a stage that covers reads on their way, so a wavefront waits for its reads in front of the barrier.
+template <bool KEYS>
 struct Lds {
-    static constexpr int AHEAD = KEYS && NT == 1 ? 1 : 2;
-    static constexpr bool DRAIN = KEYS && NT == 1;
-    static constexpr int N1 = KEYS ? AHEAD + 2 : AHEAD + 3, N2 = KEYS && !DRAIN ? AHEAD + 2 : AHEAD + 1, NF = AHEAD + 1;    // stages of Y1, Y2, figures
-    static constexpr int Y2 = N1 * TILE_BYTES, X2 = Y2 + N2 * TILE_BYTES, FIGURES = X2 + (KEYS ? 4 * NT * 32 * ROW_BYTES : 0);
+    static constexpr int AHEAD = KEYS ? 1 : 2;
+    static constexpr bool DRAIN = KEYS;
+    static constexpr int N1 = KEYS ? AHEAD + 2 : AHEAD + 3, N2 = AHEAD + 1, NF = AHEAD + 1;       // stages of Y1, Y2, figures
+    static constexpr int Y2 = N1 * TILE_BYTES, X2 = Y2 + N2 * TILE_BYTES, FIGURES = X2 + (KEYS ? 4 * 32 * ROW_BYTES : 0);
     static constexpr int BYTES = FIGURES + (KEYS ? NF * STATS_BYTES : 0);
 };
-constexpr int lds_bytes(int nt)
+constexpr int LDS_BYTES = Lds<true>::BYTES > Lds<false>::BYTES ? Lds<true>::BYTES : Lds<false>::BYTES;
+static_assert(LDS_BYTES <= 80 * 1024);
+
+// n / d for n < 2^31 with constants found on the host
+struct Div { uint32_t mul, shift; };
+__host__ inline Div make_div(uint32_t d)
 {
-    const int keys = nt == 1 ? Lds<true, 1>::BYTES : Lds<true, 2>::BYTES, rows = nt == 1 ? Lds<false, 1>::BYTES : Lds<false, 2>::BYTES;
-    return keys > rows ? keys : rows;
+    uint32_t l = 0;
+    while ((1ull << l) < d) ++l;
+    return {(uint32_t)(((1ull << 32) * ((1ull << l) - d)) / d + 1), l};
 }
-static_assert(lds_bytes(2) <= 160 * 1024 && lds_bytes(1) <= 80 * 1024);
+__device__ __forceinline__ int fast_div(int n, Div d) { return (int)((__umulhi((uint32_t)n, d.mul) + (uint32_t)n) >> d.shift); }
 
 // The items of one kind.  A tile's steps (streamed tiles, of all heads of a group) are cut into pieces of at most `most`, so that a call of few or
 // uneven tiles fills the chip; a tile of several pieces leaves FP32 parts, which attn_bwd_join adds up.
 struct Role {
     int groups, tiles, splits;      // grid: groups x tiles x splits (the largest number of pieces)
     int most;
-    int window;                     // groups of an XCD whose tiles are dealt out together; 0: XCDs are not told apart
+    int window;                     // groups whose tiles are dealt out together
+    bool by_xcd;                    // an XCD keeps to its own groups
     int items;
+    Div d_window, d_per_tile, d_per_window;
 };
 struct Params {
     const __bf16 *q, *k, *v, *dout;
@@ -81,10 +90,11 @@ struct Params {
     const float *stats;
     float *part_q, *part_kv;        // parts: [split][rows of dq] / [split][dk or dv][rows]
     int B, Hq, Hkv, Sq, Skv, G, qtiles;
-    int pack, chunks;               // rows items: query heads of a group side by side, and how many such chunks a group has
+    int pack_log2, chunks;          // rows items: query heads of a group side by side, and how many such chunks a group has
     int off;                        // key j valid for row i iff j <= i + off (without the mask: always true)
     float c, scale;                 // c = scale * log2(e)
     Role keys, rows;
+    Div d_hkv, d_chunks;
 };
 
 // f(0), f(1), ... f(N - 1) with constants (the unroller gives up on a loop of this size)
@@ -94,14 +104,15 @@ template <int N, class F>
 __device__ __forceinline__ void static_for(F &&f) { static_for(std::make_integer_sequence<int, N>{}, f); }
 
 // Query tiles in front of a tile's first key (keys items); steps of a tile.
-__host__ __device__ inline int keys_skip(const Params &p, int tile, int nt)
+__host__ __device__ inline int keys_skip(const Params &p, int tile)
 {
-    const int first = tile * (128 * nt) - p.off;        // first row that sees the tile's first key
+    const int first = tile * ITEM_ROWS - p.off;             // first row that sees the tile's first key
     return first > 0 ? (first / BT < p.qtiles ? first / BT : p.qtiles) : 0;
 }
-__host__ __device__ inline int rows_steps(const Params &p, int tile, int nt)
+__host__ __device__ inline int keys_steps(const Params &p, int tile) { return (p.qtiles - keys_skip(p, tile)) * p.G; }
+__host__ __device__ inline int rows_steps(const Params &p, int tile)
 {
-    const int end = (tile + 1) * (128 * nt / p.pack);
+    const int end = (tile + 1) * (ITEM_ROWS >> p.pack_log2);
     const int last = (end < p.Sq ? end : p.Sq) - 1 + p.off;      // last key that the tile's last row sees
     return last < 0 ? 0 : (last < p.Skv - 1 ? last : p.Skv - 1) / BT + 1;
 }
@@ -133,16 +144,6 @@ __device__ __forceinline__ void lds_dma4(const unsigned char *base, uint32_t vof
                  : "memory", "m0");
 }
 #pragma clang diagnostic pop
-// acc += A B for the sums that a wavefront keeps through all steps, in the accumulation half of the register file (the compiler, which
-// gives all products of a kernel one form or moves them between the halves as it sees fit, otherwise copies up to 300 registers a step).
-// It knows nothing of the instruction's timing, so: between a vector-ALU instruction that writes A or B and the product that reads it stand two others
-// (a host-side test looks for it in the built code; LDS reads the compiler waits for); and nothing but the same kind of product reads `acc` until
-// acc_ready(), two into the same registers being 4 * NT products apart.
-__device__ __forceinline__ void mfma_acc(f32x16 &acc, bf16x8 a, bf16x8 b) {
-    asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
-}
-// 16 passes at most, so 18 wait states between a product and another instruction that reads its result
-__device__ __forceinline__ void acc_ready(f32x16 &acc) { asm volatile("s_nop 15\n\ts_nop 3" : "+a"(acc)); }
 constexpr int wait_vmcnt(int n) { return 0x0F70 | n; }     // s_waitcnt vmcnt(n), n < 16
 constexpr int WAIT_LGKMCNT0 = ~0x0F00;                      // (and it also waits for this wavefront's LDS reads)
 __device__ __forceinline__ void wg_barrier() {
@@ -206,11 +207,11 @@ __global__ __launch_bounds__(256) void attn_bwd_stats(const __bf16 *dout, const 
 }
 
 // ------------------------------------------------------------------------------------------------------ the products
-// One item: KEYS holds K (X1), V (X2) and streams Q (Y1), dO (Y2); otherwise the reverse.  NT: held 32-row tiles per wavefront.
-template <bool KEYS, int NT>
+// One item: KEYS holds K (X1), V (X2) and streams Q (Y1), dO (Y2); otherwise the reverse.
+template <bool KEYS>
 __device__ __forceinline__ void item(const Params &p, int group, int tile, int piece)
 {
-    typedef Lds<KEYS, NT> L;
+    typedef Lds<KEYS> L;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     LDS_AS unsigned char *lds = (LDS_AS unsigned char *)smem;
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
@@ -220,28 +221,31 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     // ---- what this wavefront holds, and the steps that it streams
     int b, x_head, x0, x_rows, y_rows, y_head0;
     if (KEYS) {
-        b = group / p.Hkv;
+        b = fast_div(group, p.d_hkv);
         x_head = group - b * p.Hkv;
-        x0 = tile * (128 * NT) + wave * 32 * NT;
+        x0 = tile * ITEM_ROWS + wave * 32;
         x_rows = p.Skv;
         y_rows = p.Sq;
         y_head0 = x_head * p.G;
     } else {
-        const int bh = group / p.chunks;
-        b = bh / p.Hkv;
+        const int bh = fast_div(group, p.d_chunks);
+        b = fast_div(bh, p.d_hkv);
         y_head0 = bh - b * p.Hkv;
-        x_head = y_head0 * p.G + (group - bh * p.chunks) * p.pack + (wave & (p.pack - 1));
-        x0 = tile * (128 * NT / p.pack) + (wave / p.pack) * 32 * NT;
+        x_head = y_head0 * p.G + ((group - bh * p.chunks) << p.pack_log2) + (wave & ((1 << p.pack_log2) - 1));
+        x0 = tile * (ITEM_ROWS >> p.pack_log2) + (wave >> p.pack_log2) * 32;
         x_rows = p.Sq;
         y_rows = p.Skv;
     }
     // KEYS: query tiles t0 .. qtiles - 1 of each head; else: key tiles from 0 on
-    const int t0 = KEYS ? keys_skip(p, tile, NT) : 0;
-    const int per_head = KEYS ? p.qtiles - t0 : rows_steps(p, tile, NT);
-    const int tile_steps = KEYS ? per_head * p.G : per_head, n_pieces = pieces(tile_steps, KEYS ? p.keys.most : p.rows.most);
+    const int t0 = KEYS ? keys_skip(p, tile) : 0;
+    const int per_head = KEYS ? p.qtiles - t0 : rows_steps(p, tile);
+    int steps = KEYS ? per_head * p.G : per_head, step0 = 0;
+    const int n_pieces = pieces(steps, KEYS ? p.keys.most : p.rows.most);
     if (piece >= n_pieces) return;
-    const int step0 = (int)((long long)tile_steps * piece / n_pieces);
-    int steps = (int)((long long)tile_steps * (piece + 1) / n_pieces) - step0;
+    if (n_pieces > 1) {
+        step0 = (int)((unsigned)steps * (unsigned)piece / (unsigned)n_pieces);
+        steps = (int)((unsigned)steps * (unsigned)(piece + 1) / (unsigned)n_pieces) - step0;
+    }
     // (all of it is wave-uniform: scalar registers)
     auto uniform = [](int &x) __attribute__((always_inline)) { x = __builtin_amdgcn_readfirstlane(x); };
     uniform(b); uniform(x_head); uniform(x0); uniform(y_head0); uniform(steps);
@@ -254,7 +258,7 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     struct At { int tile, head, s1, s2, sf; };
     const int y_tiles = KEYS ? p.qtiles : (y_rows + BT - 1) / BT;
     At cur, req;
-    cur.head = KEYS && per_head > 0 ? step0 / per_head : 0;
+    cur.head = KEYS && step0 > 0 ? step0 / per_head : 0;
     cur.tile = KEYS ? min(step0 - cur.head * per_head + t0, y_tiles - 1) : min(step0, y_tiles - 1);
     uniform(cur.head);
     uniform(cur.tile);
@@ -311,47 +315,38 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     };
 
     // ---- held operands
-    bf16x8 x1[NT][8], x2[NT][8];
-    f32x16 nd[NT];              // rows items: -delta of the lane's row in every element, the C operand that dP starts from
-    float nl[NT];
-    const uint32_t x2_at = lds0 + L::X2 + wave * (NT * 32 * ROW_BYTES);
-    {
-        const __bf16 *xg1 = KEYS ? p.k : p.q, *xg2 = KEYS ? p.v : p.dout;
+    const uint32_t x2_at = lds0 + L::X2 + wave * (32 * ROW_BYTES);
+    bf16x8 x1[8], x2[8];
+    f32x16 nd;              // rows items: -delta of the lane's row in every element, the C operand that dP starts from
+    float nl = 0.0f;
+    const bool dead = x0 >= x_rows;     // this wavefront's rows lie behind the last one
+    if (!dead) {
+        const __bf16 *from1 = KEYS ? p.k : p.q, *from2 = KEYS ? p.v : p.dout;
+        const int row = min(x0 + l32, x_rows - 1);
+        const size_t at = ((size_t)((size_t)b * x_rows + row) * x_heads + x_head) * HD + 8 * hh;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int row = min(x0 + 32 * t + l32, x_rows - 1);
-            const size_t at = ((size_t)((size_t)b * x_rows + row) * x_heads + x_head) * HD + 8 * hh;
+        for (int s = 0; s < 8; ++s) x1[s] = *(const bf16x8 *)(from1 + at + 16 * s);
+        if (KEYS) {         // (V in registers as well: no room beside K, two accumulators of its size and the scores.)  In the order of
+                            // its fragments, lane by lane: reads are one address and a constant.
+            const unsigned char *g = uniform_ptr((const unsigned char *)(from2 + ((size_t)((size_t)b * x_rows + x0) * x_heads + x_head) * HD));
+            const uint32_t o = (uint32_t)(row - x0) * (uint32_t)(x_heads * ROW_BYTES) + 16 * hh;
 #pragma unroll
-            for (int s = 0; s < 8; ++s) x1[t][s] = *(const bf16x8 *)(xg1 + at + 16 * s);
-            if (!KEYS) {
+            for (int i = 0; i < 8; ++i) lds_dma16(g, o + 32 * i, __builtin_amdgcn_readfirstlane(x2_at + i * 1024));
+        } else {
 #pragma unroll
-                for (int s = 0; s < 8; ++s) x2[t][s] = *(const bf16x8 *)(xg2 + at + 16 * s);
-                const int i = min(x0 + 32 * t + l32, p.Sq - 1);
-                const float *st = p.stats + ((size_t)((size_t)b * p.Hq + x_head) * p.qtiles + (i >> 5)) * (2 * BT) + (i & 31);
-                nl[t] = st[0];
-                const float d = st[BT];
+            for (int s = 0; s < 8; ++s) x2[s] = *(const bf16x8 *)(from2 + at + 16 * s);
+            const float *st = p.stats + ((size_t)((size_t)b * p.Hq + x_head) * p.qtiles + (row >> 5)) * (2 * BT) + (row & 31);
+            nl = st[0];
+            const float d = st[BT];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) nd[t][r] = d;
-            }
-        }
-        if (KEYS) {             // (V in registers as well: no room beside K, two accumulators of its size and the scores)
-            const int first = min(x0, x_rows - 1), last = x_rows - 1 - first;
-            const unsigned char *g = uniform_ptr((const unsigned char *)(xg2 + ((size_t)((size_t)b * x_rows + first) * x_heads + x_head) * HD));
-#pragma unroll
-            for (int i = 0; i < 8 * NT; ++i) {
-                const int row = 4 * i + ld_r;
-                lds_dma16(g, (uint32_t)min(row, last) * (uint32_t)(x_heads * ROW_BYTES) + ((ld_u ^ swz(row)) << 4),
-                          __builtin_amdgcn_readfirstlane(x2_at + i * 1024));
-            }
+            for (int r = 0; r < 16; ++r) nd[r] = d;
         }
     }
-    f32x16 acc1[NT][4], acc2[NT][4];
+    f32x16 acc1[4], acc2[4];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc1[t][d][r] = acc2[t][d][r] = 0.0f;
+        for (int r = 0; r < 16; ++r) acc1[d][r] = acc2[d][r] = 0.0f;
 
     // ---- LDS reads.  Row l32, unit 2 s + hh: as the swizzle is an exclusive or and tiles are 256-byte aligned, that is the address of
     // unit hh with s << 5 flipped.  Transposed: row 4 hh + i / 4 (+ 8 e, + 16 k) and four d's: likewise with d << 6 and e << 5 flipped.
@@ -362,36 +357,34 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
         t_at = row * ROW_BYTES + (((col >> 3) ^ swz(row)) << 4) + (col & 7) * 2;
     }
     typedef const LDS_AS unsigned char *Ptr;
-    auto row_frag = [&](uint32_t at, int s, int imm) __attribute__((always_inline)) -> bf16x8 {     // `at`: r_at in the stage
-        return *(const LDS_AS bf16x8 *)((Ptr)(uintptr_t)(at ^ (s << 5)) + imm);
+    auto row_frag = [&](uint32_t tile_at, int s) __attribute__((always_inline)) -> bf16x8 {
+        return *(const LDS_AS bf16x8 *)(Ptr)(uintptr_t)((lds0 + tile_at + r_at) ^ (s << 5));
     };
-    auto col_frag = [&](uint32_t at, int k, int d, int imm) __attribute__((always_inline)) -> bf16x8 {     // `at`: t_at in the stage
-        s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Ptr)(uintptr_t)(at ^ (d << 6)) + (imm + 16 * k * ROW_BYTES)));
-        s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Ptr)(uintptr_t)(at ^ (d << 6) ^ 32) + (imm + (16 * k + 8) * ROW_BYTES)));
+    auto col_frag = [&](uint32_t tile_at, int k, int d) __attribute__((always_inline)) -> bf16x8 {
+        const uint32_t at = (lds0 + tile_at + t_at) ^ (d << 6);
+        s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Ptr)(uintptr_t)at + 16 * k * ROW_BYTES));
+        s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Ptr)(uintptr_t)(at ^ 32) + (16 * k + 8) * ROW_BYTES));
         s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
         return __builtin_bit_cast(bf16x8, v);
     };
 
-    // ---- a step: phases of 8 operand fragments of Y, each fragment for NT products,
+    // ---- a step: phases of 8 products, each with an operand fragment of Y,
     //     KEYS:  S(j)   acc1 += Y1^T dS(j-1)   dP(j)   acc2 += Y2^T P(j)
     //     rows:  S(j)   dP(j)   acc1 += Y1^T dS(j-1)
     // and between the products the vector work, each piece a phase or two after the products that it needs: rounding dS(j-1) during S(j), the
-    // exponents of S(j) during the two phases after it, P * dP behind dP(j).  Fragments are read LEAD ahead, across the end of
-    // a step too, so the step's barrier stands LEAD fragments before its end.
-    constexpr int LEAD = NT == 2 ? 3 : 2, LEAD2 = NT == 2 ? 2 : 1;      // (NT = 1: the other workgroup of the compute unit hides more)
-    constexpr int NF = KEYS ? 32 : 24;          // fragments of a step; fragment f lies in frag[f % 4]
+    // exponents of S(j) during the two phases after it, P * dP behind dP(j).  Fragments are read LEAD products ahead, across the end of
+    // a step too, so the step's barrier stands LEAD products before its end.
+    constexpr int LEAD = 2;
+    constexpr int NF = KEYS ? 32 : 24;          // products of a step; fragment f lies in frag[f % 4]
     static_assert(LEAD < 4 && NF % 4 == 0);
     constexpr int PH_S = 0, PH_DP = KEYS ? 2 : 1, PH_1 = KEYS ? 1 : 2, PH_2 = 3;
-    constexpr int SLOTS = 8 * NT;               // products of a phase
-    bf16x8 frag[4], frag2[LEAD2 + 1][NT];
-    f32x16 s[NT], dp[NT];
-    u32x4 pb[NT][2], ds[NT][2];                 // BF16 pairs, the B operands of acc2 and acc1
+    bf16x8 frag[4], frag2[2];
+    f32x16 s, dp;
+    u32x4 pb[2], ds[2];                         // BF16 pairs, the B operands of acc2 and acc1
     int prev1 = 0;                              // stage of step j - 1's Y1
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dp[t][r] = 0.0f;
-    // (held in place as soon as it is complete: moved behind other instructions it could end up right in front of its product)
+    for (int r = 0; r < 16; ++r) dp[r] = 0.0f;
+    // (held in place once four are complete: the compiler otherwise keeps twice as many FP32 values and rounds them right in front of a product)
     auto pack = [&](u32x4 (&w)[2], int r, float x0, float x1) __attribute__((always_inline)) {       // elements r, r + 1
         w[r >> 3][(r >> 1) & 3] = pack_bf16(x0, x1);
         if ((r & 7) == 6) asm volatile("" : "+v"(w[r >> 3]));
@@ -399,59 +392,40 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     auto fetch = [&](int f) __attribute__((always_inline)) {
         const int ph = f >> 3, i = f & 7;
         bf16x8 &to = frag[f % 4];
-        if (f >= NF) to = row_frag(lds0 + next1(cur.s1) + r_at, i, 0);
-        else if (ph == PH_S) to = row_frag(lds0 + cur.s1 + r_at, i, 0);
-        else if (ph == PH_DP) to = row_frag(lds0 + cur.s2 + r_at, i, 0);
-        else if (ph == PH_1) to = col_frag(lds0 + prev1 + t_at, i >> 2, i & 3, 0);
-        else to = col_frag(lds0 + cur.s2 + t_at, i >> 2, i & 3, 0);
+        if (f >= NF) to = row_frag(next1(cur.s1), i);
+        else if (ph == PH_S) to = row_frag(cur.s1, i);
+        else if (ph == PH_DP) to = row_frag(cur.s2, i);
+        else if (ph == PH_1) to = col_frag(prev1, i >> 2, i & 3);
+        else to = col_frag(cur.s2, i >> 2, i & 3);
     };
-    auto fetch2 = [&](int f) __attribute__((always_inline)) {
-        const int i = f & 7;
-        if (KEYS && f < NF && (f >> 3) == PH_DP) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t) frag2[i % (LEAD2 + 1)][t] = row_frag(x2_at + r_at, i, t * 32 * ROW_BYTES);
-        }
-    };
-    const int x_last = min(x0 + 32 * NT, x_rows) - 1;
     auto step = [&]() __attribute__((always_inline)) {
         const int y0 = cur.tile * BT;
-        const bool masked = KEYS ? x_last > y0 + p.off : (y0 + BT - 1 > x0 + p.off || y0 + BT > y_rows);
+        const bool masked = KEYS ? min(x0 + 32, x_rows) - 1 > y0 + p.off : (y0 + BT - 1 > x0 + p.off || y0 + BT > y_rows);
         const Ptr figures = (Ptr)(uintptr_t)(lds0 + cur.sf) + 16 * hh;
         f32x4 nlv[4];
         // Masked pairs (KEYS: row < key - off; else key > row + off or key >= Skv) give exactly 0, whatever they hold.  A branch around
         // selects alone: two forms of the whole step meet in copies of hundreds of registers.
         auto mask = [&](auto &&f) __attribute__((always_inline)) {
             if (masked) {
+                int ln = lane;
+                asm volatile("" : "+v"(ln));        // formed here, not kept through all steps
+                const int x = x0 + (ln & 31), lim = (KEYS ? x - p.off : min(x + p.off, p.Skv - 1)) - y0 - 4 * (ln >> 5);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    int ln = lane;
-                    asm volatile("" : "+v"(ln));        // formed here, not kept through all steps
-                    const int x = x0 + 32 * t + (ln & 31);
-                    const int lim = (KEYS ? x - p.off : min(x + p.off, p.Skv - 1)) - y0 - 4 * (ln >> 5);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int y = 8 * (r >> 2) + (r & 3);
-                        f(t, r, KEYS ? y >= lim : y <= lim);
-                    }
+                for (int r = 0; r < 16; ++r) {
+                    const int y = 8 * (r >> 2) + (r & 3);
+                    f(r, KEYS ? y >= lim : y <= lim);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
         };
         // element e of the vector work
-        auto do_round = [&](int e) __attribute__((always_inline)) {       // dS(j-1), pairs
-            const int t = e >> 3, r = 2 * (e & 7);
-            pack(ds[t], r, dp[t][r], dp[t][r + 1]);
-        };
+        auto do_round = [&](int e) __attribute__((always_inline)) { pack(ds, 2 * e, dp[2 * e], dp[2 * e + 1]); };
         auto do_exp = [&](int e) __attribute__((always_inline)) {
-            const int t = e >> 4, r = e & 15;
-            s[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], p.c, KEYS ? nlv[r >> 2][r & 3] : nl[t]));
-            if (KEYS && (r & 1)) pack(pb[t], r - 1, s[t][r - 1], s[t][r]);
+            s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], p.c, KEYS ? nlv[e >> 2][e & 3] : nl));
+            if (KEYS && (e & 1)) pack(pb, e - 1, s[e - 1], s[e]);
         };
-        auto do_mul = [&](int e) __attribute__((always_inline)) {
-            const int t = e >> 4, r = e & 15;
-            dp[t][r] = s[t][r] * dp[t][r];
-        };
-        // pieces lo .. hi of n that belong to slot `k` of `of`
+        auto do_mul = [&](int e) __attribute__((always_inline)) { dp[e] *= s[e]; };
+        // the n elements dealt out evenly to `of` slots: those of slot k
         auto spread = [&](int k, int of, int n, auto &&f) __attribute__((always_inline)) {
             if (k < 0 || k >= of) return;
 #pragma unroll
@@ -461,12 +435,10 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
         static_for<NF>([&](auto fc) __attribute__((always_inline)) {
             constexpr int f = decltype(fc)::value, ph = f >> 3, i = f & 7;
             if constexpr (KEYS && f == 8 * PH_2) {
-                mask([&](int t, int r, bool ok) __attribute__((always_inline)) {
-                    s[t][r] = ok ? s[t][r] : 0.0f;
-                    if (r & 1) pack(pb[t], r - 1, s[t][r - 1], s[t][r]);
+                mask([&](int r, bool ok) __attribute__((always_inline)) {
+                    s[r] = ok ? s[r] : 0.0f;
+                    if (r & 1) pack(pb, r - 1, s[r - 1], s[r]);
                 });
-                asm volatile("s_nop 1");
-                __builtin_amdgcn_sched_barrier(0);
             }
             if (f == NF - LEAD) {
                 // the next step's tiles have landed (all but those of the steps behind it), for every wavefront
@@ -474,48 +446,35 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
                 wg_barrier();
             }
             fetch(f + LEAD);
-            fetch2(f + LEAD2);
+            if constexpr (KEYS && ((f + 1) >> 3) == PH_DP) frag2[(f + 1) & 1] = *(const LDS_AS bf16x8 *)((Ptr)(uintptr_t)(x2_at + lane * 16) + ((f + 1) & 7) * 1024);
             if (f >= 1 && f <= PER_STEP) request_part(f - 1);
             if (f == PER_STEP + 1) request_done();
-            if constexpr (KEYS) {       // -LSE, a quarter at a time shortly before its exponents (NT = 2: used twice, kept); -delta, where dP starts from
-                constexpr int g = NT == 2 ? f - 4 : (f - 6) / 3;
-                if constexpr (NT == 2 ? g >= 0 && g < 4 : f >= 6 && (f - 6) % 3 == 0 && g < 4) nlv[g] = *(const LDS_AS f32x4 *)(figures + 32 * g);
-                if constexpr (f >= 8 && f < 12) {
-                    const f32x4 d = *(const LDS_AS f32x4 *)(figures + BT * 4 + 32 * (f - 8));
+            // -LSE, a quarter at a time shortly before its exponents; -delta, where dP starts from
+            if constexpr (KEYS && f >= 6 && f < 18 && (f - 6) % 3 == 0) nlv[(f - 6) / 3] = *(const LDS_AS f32x4 *)(figures + 32 * ((f - 6) / 3));
+            if constexpr (KEYS && f >= 8 && f < 12) {
+                const f32x4 d = *(const LDS_AS f32x4 *)(figures + BT * 4 + 32 * (f - 8));
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) dp[t][4 * (f - 8) + e] = d[e];
-                }
+                for (int e = 0; e < 4; ++e) dp[4 * (f - 8) + e] = d[e];
             }
             const bf16x8 a = frag[f % 4];
-            static_for<NT>([&](auto tc) __attribute__((always_inline)) {
-                constexpr int t = decltype(tc)::value;
-                if constexpr (ph == PH_S) {
-                    f32x16 zero;
+            if constexpr (ph == PH_S) {
+                f32x16 zero;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
-                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, x1[t][i], i == 0 ? zero : s[t], 0, 0, 0);
-                } else if constexpr (ph == PH_DP) {
-                    dp[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, KEYS ? frag2[i % (LEAD2 + 1)][t] : x2[t][i], !KEYS && i == 0 ? nd[t] : dp[t], 0, 0, 0);
-                } else if constexpr (ph == PH_1) {
-                    mfma_acc(acc1[t][i & 3], a, __builtin_bit_cast(bf16x8, ds[t][i >> 2]));
-                } else {
-                    mfma_acc(acc2[t][i & 3], a, __builtin_bit_cast(bf16x8, pb[t][i >> 2]));
-                }
-                constexpr int slot = f * NT + t;
-                spread(slot, SLOTS, 8 * NT, do_round);
-                if (KEYS) {
-                    spread(slot - SLOTS - NT, 2 * SLOTS - NT, 16 * NT, do_exp);
-                    spread(slot - 3 * SLOTS - NT, SLOTS - NT, 16 * NT, do_mul);
-                } else {
-                    spread(slot - SLOTS - NT, SLOTS + SLOTS / 2 - NT, 16 * NT, do_exp);
-                    spread(slot - 2 * SLOTS - NT, SLOTS - NT, 16 * NT, do_mul);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            });
+                for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, x1[i], i == 0 ? zero : s, 0, 0, 0);
+            } else if constexpr (ph == PH_DP) {
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, KEYS ? frag2[i & 1] : x2[i], !KEYS && i == 0 ? nd : dp, 0, 0, 0);
+            } else if constexpr (ph == PH_1) {
+                acc1[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, ds[i >> 2]), acc1[i & 3], 0, 0, 0);
+            } else {
+                acc2[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, pb[i >> 2]), acc2[i & 3], 0, 0, 0);
+            }
+            spread(f, 8, 8, do_round);
+            spread(f - 9, KEYS ? 15 : 11, 16, do_exp);
+            spread(f - (KEYS ? 25 : 17), 7, 16, do_mul);
+            __builtin_amdgcn_sched_barrier(0);
         });
-        mask([&](int t, int r, bool ok) __attribute__((always_inline)) { dp[t][r] = ok ? dp[t][r] : 0.0f; });
+        mask([&](int r, bool ok) __attribute__((always_inline)) { dp[r] = ok ? dp[r] : 0.0f; });
         prev1 = cur.s1;
         next_stages(cur);
         if (KEYS && cur.tile == y_tiles - 1) cur.tile = t0;
@@ -531,62 +490,55 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
         // (all of them, so that the compiler, which counts the loads above but not these, has none left to wait for in the loop)
         __builtin_amdgcn_s_waitcnt(0);
         wg_barrier();
+        if (dead) {             // its share of the requests, and the barriers
+            for (int j = 0; j < steps; ++j) {
+#pragma unroll
+                for (int n = 0; n < PER_STEP; ++n) request_part(n);
+                request_done();
+                __builtin_amdgcn_s_waitcnt(wait_vmcnt((L::AHEAD - 1) * PER_STEP));
+                wg_barrier();
+            }
+            __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+            return;
+        }
 #pragma unroll
         for (int f = 0; f < LEAD; ++f) fetch(f);
         for (int j = 0; j < steps; ++j) step();
         __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
         // the last step's dS
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int r = 0; r < 16; r += 2) pack(ds, r, dp[r], dp[r + 1]);
 #pragma unroll
-            for (int r = 0; r < 16; r += 2) pack(ds[t], r, dp[t][r], dp[t][r + 1]);
-        __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_nop 1");
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const bf16x8 a = col_frag(lds0 + prev1 + t_at, i >> 2, i & 3, 0);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) mfma_acc(acc1[t][i & 3], a, __builtin_bit_cast(bf16x8, ds[t][i >> 2]));
-        }
+        for (int i = 0; i < 8; ++i)
+            acc1[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag(prev1, i >> 2, i & 3), __builtin_bit_cast(bf16x8, ds[i >> 2]), acc1[i & 3], 0, 0, 0);
     }
 
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-            acc_ready(acc1[t][d]);
-            if (KEYS) acc_ready(acc2[t][d]);
-        }
     // ---- results: lane = held row, registers 4 d's; exchanged with lane ^ 32, eight in line
-    auto store = [&](f32x16 (&acc)[NT][4], float f, __bf16 *out, float *part) __attribute__((always_inline)) {
+    const int row = x0 + l32;
+    const bool valid = row < x_rows;
+    const size_t at = ((size_t)((size_t)b * x_rows + (valid ? row : 0)) * x_heads + x_head) * HD;
+    auto store = [&](f32x16 (&acc)[4], float f, __bf16 *out, float *part) __attribute__((always_inline)) {
+        if (n_pieces == 1) {
+            unsigned char *op = (unsigned char *)(out + at + 8 * hh);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int row = x0 + 32 * t + l32;
-            const bool valid = row < x_rows;
-            const size_t at = ((size_t)((size_t)b * x_rows + (valid ? row : 0)) * x_heads + x_head) * HD;
-            if (n_pieces == 1) {
-                unsigned char *op = (unsigned char *)(out + at + 8 * hh);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const f32x16 &a = acc[t][i >> 1];
-                    const int e = 8 * (i & 1);
-                    auto u = __builtin_amdgcn_permlane32_swap(pack_bf16(a[e] * f, a[e + 1] * f), pack_bf16(a[e + 4] * f, a[e + 5] * f), false, false);
-                    auto w = __builtin_amdgcn_permlane32_swap(pack_bf16(a[e + 2] * f, a[e + 3] * f), pack_bf16(a[e + 6] * f, a[e + 7] * f), false, false);
-                    const u32x4 ww = {u[0], w[0], u[1], w[1]};
-                    if (valid) *(u32x4 *)(op + 32 * i) = ww;
-                }
-            } else if (valid) {
-                float *op = part + at + 4 * hh;
-#pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const f32x16 &a = acc[t][d];
-                        const f32x4 y = {a[4 * g] * f, a[4 * g + 1] * f, a[4 * g + 2] * f, a[4 * g + 3] * f};
-                        *(f32x4 *)(op + 32 * d + 8 * g) = y;
-                    }
+            for (int i = 0; i < 8; ++i) {
+                const f32x16 &a = acc[i >> 1];
+                const int e = 8 * (i & 1);
+                auto u = __builtin_amdgcn_permlane32_swap(pack_bf16(a[e] * f, a[e + 1] * f), pack_bf16(a[e + 4] * f, a[e + 5] * f), false, false);
+                auto w = __builtin_amdgcn_permlane32_swap(pack_bf16(a[e + 2] * f, a[e + 3] * f), pack_bf16(a[e + 6] * f, a[e + 7] * f), false, false);
+                const u32x4 ww = {u[0], w[0], u[1], w[1]};
+                if (valid) *(u32x4 *)(op + 32 * i) = ww;
             }
+        } else if (valid) {
+            float *op = part + at + 4 * hh;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x16 &a = acc[d];
+                    const f32x4 y = {a[4 * g] * f, a[4 * g + 1] * f, a[4 * g + 2] * f, a[4 * g + 3] * f};
+                    *(f32x4 *)(op + 32 * d + 8 * g) = y;
+                }
         }
     };
     const size_t all = (size_t)p.B * x_rows * x_heads * HD;
@@ -603,38 +555,33 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
 // the tiles of a group, which stream the same data, meet in one L2.
 __device__ __forceinline__ void find_item(const Role &r, int n, int &group, int &tile, int &piece)
 {
-    int width = r.groups, base = 0, at = n;
-    if (r.window) {
-        const int per_xcd = r.groups >> 3, per_window = r.window * r.tiles * r.splits;
-        at = n >> 3;
-        const int w = at / per_window;
-        at -= w * per_window;
-        width = min(r.window, per_xcd - w * r.window);
-        base = (n & 7) * per_xcd + w * r.window;
+    int base = 0;
+    if (r.by_xcd) {
+        base = (n & 7) * (r.groups >> 3);
+        n >>= 3;
     }
-    const int per_tile = width * r.splits;
-    tile = at / per_tile;
-    at -= tile * per_tile;
-    piece = at / width;
-    group = base + at - piece * width;
+    const int w = fast_div(n, r.d_per_window);
+    n -= w * r.window * r.tiles * r.splits;
+    tile = fast_div(n, r.d_per_tile);
+    n -= tile * r.window * r.splits;
+    piece = fast_div(n, r.d_window);
+    group = base + w * r.window + n - piece * r.window;
 }
 
-template <int NT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3 - NT, 3 - NT))) void attn_bwd_kernel(const Params p)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_bwd_kernel(const Params p)
 {
     const int n = blockIdx.x;
     int group, tile, piece;
     if (n < p.keys.items) {
         find_item(p.keys, n, group, tile, piece);
-        item<true, NT>(p, group, tile, piece);
+        item<true>(p, group, tile, piece);
     } else {
         find_item(p.rows, n - p.keys.items, group, tile, piece);
-        item<false, NT>(p, group, p.rows.tiles - 1 - tile, piece);
+        item<false>(p, group, p.rows.tiles - 1 - tile, piece);
     }
 }
 
 // The sum of the parts of each tile that was cut, in the order of its pieces: 8 elements per thread, first those of dk and dv, then of dq.
-template <int NT>
 __global__ __launch_bounds__(256) void attn_bwd_join(const Params p, uint32_t kv_blocks)
 {
     const bool keys = blockIdx.x < kv_blocks;
@@ -643,14 +590,7 @@ __global__ __launch_bounds__(256) void attn_bwd_join(const Params p, uint32_t kv
     const size_t i = ((size_t)(blockIdx.x - (keys ? 0 : kv_blocks)) * 256 + threadIdx.x) * 8;
     if (i >= all) return;
     const int pos = (int)((i / HD / H) % S);
-    int n;
-    if (keys) {
-        const int tile = pos / (128 * NT);
-        n = pieces((p.qtiles - keys_skip(p, tile, NT)) * p.G, p.keys.most);
-    } else {
-        const int tile = pos / (128 * NT / p.pack);
-        n = pieces(rows_steps(p, tile, NT), p.rows.most);
-    }
+    const int n = keys ? pieces(keys_steps(p, pos / ITEM_ROWS), p.keys.most) : pieces(rows_steps(p, pos / (ITEM_ROWS >> p.pack_log2)), p.rows.most);
     if (n == 1) return;
     auto sum = [&](const float *part, size_t stride, __bf16 *out) {
         f32x4 a = {0, 0, 0, 0}, c = {0, 0, 0, 0};
@@ -673,7 +613,6 @@ __global__ __launch_bounds__(256) void attn_bwd_join(const Params p, uint32_t kv
 
 // ----------------------------------------------------------------------------------------------------------- host
 struct Plan {
-    int nt;
     Params p;                                   // sizes and roles
     size_t stats, part_kv, part_q, total;       // bytes: the workspace's three parts
 };
@@ -687,20 +626,32 @@ int check_sizes(int B, int Hq, int Hkv, int Sq, int Skv, int D)
     return ATTN_OK;
 }
 
-constexpr int CUS = 256;        // of the device that this is written for: how items are cut (and so what the workspace needs) does not ask the device
-
-// How tiles are cut.  One workgroup is resident per compute unit.  Microseconds: what a step takes and what an item takes beside its steps.
-constexpr double KEYS_STEP = 1.6, ROWS_STEP = 1.25, ITEM = 7.0, JOIN = 4.0, JOIN_BYTES = 4.0e6;
+// Workgroups that are resident at a time on the device that this is written for, two per compute unit: how items are cut (and so what the
+// workspace needs) does not ask the device.
+constexpr int PLACES = 512;
+// Microseconds: what a step takes with both places of a compute unit taken, what an item takes beside its steps, and the launch and
+// the bytes per microsecond of adding up parts.
+constexpr double KEYS_STEP = 1.45, ROWS_STEP = 1.05, ITEM = 6.0, JOIN = 4.0, JOIN_BYTES = 4.0e6;
+constexpr int MOST_PIECES = 32;
 
 void deal(Role &r)
 {
     r.items = r.groups * r.tiles * r.splits;
-    r.window = 0;
-    if (r.groups % 8 == 0) {
-        // all groups of an XCD at once, longest tiles first, while that is few rounds; then as many as occupy its 32 compute units
+    r.by_xcd = r.groups % 8 == 0;
+    r.window = r.groups;
+    if (r.by_xcd) {
+        // all groups of an XCD at once, longest tiles first, while that is few rounds; then as many as its 64 places take, or a few more, so that
+        // windows are equal
         const int per_xcd = r.groups / 8, per_group = r.tiles * r.splits;
-        r.window = per_xcd * per_group <= 4 * CUS / 8 ? per_xcd : (CUS / 8 + per_group - 1) / per_group;
+        r.window = per_xcd;
+        if ((long long)per_xcd * per_group > 4 * PLACES / 8) {
+            r.window = (PLACES / 8 + per_group - 1) / per_group;
+            while (per_xcd % r.window) ++r.window;
+        }
     }
+    r.d_window = make_div(r.window);
+    r.d_per_tile = make_div(r.window * r.splits);
+    r.d_per_window = make_div(r.window * r.splits * r.tiles);
 }
 
 int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &r)
@@ -708,45 +659,43 @@ int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &r)
     Params &p = r.p;
     const int G = Hq / Hkv;
     p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.Sq = Sq; p.Skv = Skv; p.G = G;
-    p.pack = G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1;
-    p.chunks = G / p.pack;
+    p.pack_log2 = G % 4 == 0 ? 2 : G % 2 == 0 ? 1 : 0;
+    p.chunks = G >> p.pack_log2;
     p.qtiles = (Sq + BT - 1) / BT;
     // (i + INT32_MAX - Sq - 256 is above every key for i >= 0 and within 32 bits for the i < Sq + 256 of a tile)
     p.off = causal ? Skv - Sq : INT32_MAX - Sq - 256;
-#ifndef NTX
-#define NTX 2
-#endif
-    const int nt = r.nt = NTX;
-    const int pos = 128 * nt / p.pack, keys = 128 * nt;
-    const long long nk = (long long)B * Hkv * ((Skv + keys - 1) / keys), nr = (long long)B * Hkv * p.chunks * ((Sq + pos - 1) / pos);
-    if (nk >= (1ll << 23) || nr >= (1ll << 23) || B > 65535 || (long long)p.qtiles * BT * Hq >= (1ll << 32) - 64 ||
-        (long long)p.qtiles * G >= (1ll << 31))
+    const int pos = ITEM_ROWS >> p.pack_log2;
+    const int tk = (Skv + ITEM_ROWS - 1) / ITEM_ROWS, tr = (Sq + pos - 1) / pos;
+    const long long nk = (long long)B * Hkv * tk, nr = (long long)B * Hkv * p.chunks * tr;
+    if (nk >= (1ll << 23) || nr >= (1ll << 23) || B > 65535 || (long long)p.qtiles * BT * Hq >= (1ll << 32) - 64 || (long long)p.qtiles * G >= (1ll << 31))
         return ATTN_E_UNSUPPORTED;
-    p.keys = {B * Hkv, (Skv + keys - 1) / keys, 1, INT32_MAX, 0, 0};
-    p.rows = {B * Hkv * p.chunks, (Sq + pos - 1) / pos, 1, INT32_MAX, 0, 0};
+    p.d_hkv = make_div(Hkv);
+    p.d_chunks = make_div(p.chunks);
+    p.keys = {B * Hkv, tk, 1, INT32_MAX};
+    p.rows = {B * Hkv * p.chunks, tr, 1, INT32_MAX};
 
-    // The longest tiles and the steps of all; the calls that are worth cutting are few tiles for the chip.
-    const int long_k = (p.qtiles - keys_skip(p, 0, nt)) * G, long_r = rows_steps(p, p.rows.tiles - 1, nt);
-    if (nk + nr < 8 * CUS) {
+    // Calls of few tiles for the chip, or of uneven ones, are cut: the pair of piece lengths whose estimate is the shortest.
+    const int long_k = keys_steps(p, 0), long_r = rows_steps(p, tr - 1);
+    if (nk + nr < 4 * PLACES && (long long)long_k * MOST_PIECES < (1ll << 31)) {
         double all_k = 0, all_r = 0;
-        for (int t = 0; t < p.keys.tiles; ++t) all_k += (p.qtiles - keys_skip(p, t, nt)) * G;
-        for (int t = 0; t < p.rows.tiles; ++t) all_r += rows_steps(p, t, nt);
+        for (int t = 0; t < tk; ++t) all_k += keys_steps(p, t);
+        for (int t = 0; t < tr; ++t) all_r += rows_steps(p, t);
         all_k *= p.keys.groups;
         all_r *= p.rows.groups;
         const double kv_bytes = 2.0 * B * Skv * Hkv * HD * 4, q_bytes = (double)B * Sq * Hq * HD * 4;
         double best = INFINITY;
         int best_k = 1, best_r = 1;
-        for (int sk = 1; sk <= 32; sk += sk < 8 ? 1 : sk / 4) {
+        for (int sk = 1; sk <= MOST_PIECES; sk += sk < 8 ? 1 : sk / 4) {
             const int mk = (long_k + sk - 1) / sk;
             if (sk > 1 && mk < 3) break;
-            for (int sr = 1; sr <= 32; sr += sr < 8 ? 1 : sr / 4) {
+            for (int sr = 1; sr <= MOST_PIECES; sr += sr < 8 ? 1 : sr / 4) {
                 const int mr = (long_r + sr - 1) / sr;
                 if (sr > 1 && mr < 4) break;
                 // pieces, about: a tile has steps / most of them and half of one more, if it is cut
                 const double pk = nk + (sk > 1 ? all_k / mk - 0.5 * nk : 0), pr = nr + (sr > 1 ? all_r / mr - 0.5 * nr : 0);
                 const double ik = ITEM + KEYS_STEP * mk, ir = ITEM + ROWS_STEP * mr;
-                const double work = (all_k * KEYS_STEP + all_r * ROWS_STEP + (pk + pr) * ITEM) / CUS;
-                double us = work + 0.5 * (pk + pr > CUS ? ir : 0);
+                const double work = (all_k * KEYS_STEP + all_r * ROWS_STEP + (pk + pr) * ITEM) / PLACES;
+                double us = work + 0.5 * (pk + pr > PLACES ? ir : 0);
                 if (us < ik) us = ik;
                 if (us < ir) us = ir;
                 if (sk > 1 || sr > 1) us += JOIN + 2 * ((sk > 1 ? sk * kv_bytes : 0) + (sr > 1 ? sr * q_bytes : 0)) / JOIN_BYTES;
@@ -817,8 +766,7 @@ int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, 
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return ATTN_E_LAUNCH;
     if (!ready[dev].load(std::memory_order_acquire)) {
-        if (hipFuncSetAttribute((const void *)attn_bwd_kernel<1>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(1)) != hipSuccess ||
-            hipFuncSetAttribute((const void *)attn_bwd_kernel<2>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(2)) != hipSuccess)
+        if (hipFuncSetAttribute((const void *)attn_bwd_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES) != hipSuccess)
             return ATTN_E_LAUNCH;
         ready[dev].store(true, std::memory_order_release);
     }
@@ -841,16 +789,14 @@ int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, 
     }
     {
         void *args[] = {&p};
-        if (!launch(r.nt == 1 ? (const void *)attn_bwd_kernel<1> : (const void *)attn_bwd_kernel<2>, dim3(p.keys.items + p.rows.items), 256,
-                    lds_bytes(r.nt), args, st))
-            return ATTN_E_LAUNCH;
+        if (!launch((const void *)attn_bwd_kernel, dim3(p.keys.items + p.rows.items), 256, LDS_BYTES, args, st)) return ATTN_E_LAUNCH;
     }
     if (p.keys.splits > 1 || p.rows.splits > 1) {
         auto blocks = [](size_t n) { return (uint32_t)((n / 8 + 255) / 256); };
         uint32_t kv_blocks = p.keys.splits > 1 ? blocks((size_t)B * Skv * Hkv * HD) : 0;
         const uint32_t q_blocks = p.rows.splits > 1 ? blocks((size_t)B * Sq * Hq * HD) : 0;
         void *args[] = {&p, &kv_blocks};
-        if (!launch(r.nt == 1 ? (const void *)attn_bwd_join<1> : (const void *)attn_bwd_join<2>, dim3(kv_blocks + q_blocks), 256, 0, args, st)) return ATTN_E_LAUNCH;
+        if (!launch((const void *)attn_bwd_join, dim3(kv_blocks + q_blocks), 256, 0, args, st)) return ATTN_E_LAUNCH;
     }
     return ATTN_OK;
 }

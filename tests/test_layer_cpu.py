@@ -179,47 +179,3 @@ def test_norm_rope_reference_against_differences(interleaved):
             diff = (f(x + e, w) - f(x - e, w)) / (2 * h) if t is x else (f(x, w + e) - f(x, w - e)) / (2 * h)
             assert abs(diff - d.reshape(-1)[i]) < 1e-7
 
-
-# ---------------------------------------------------------------------------------------- the built code of the backward kernels
-def _registers(text):
-    """The vector registers that an operand names: ('v' or 'a', number)."""
-    import re
-    out = set()
-    for kind, lo, hi in re.findall(r"\b([va])\[(\d+):(\d+)\]", text):
-        out |= {(kind, n) for n in range(int(lo), int(hi) + 1)}
-    return out | {(kind, int(n)) for kind, n in re.findall(r"\b([va])(\d+)\b", text)}
-
-
-def hazards(lines):
-    """Products that read A or B fewer than two wait states behind the vector-ALU instruction that wrote it (an s_nop n stands for n + 1)."""
-    found, recent = [], []          # recent: (wait states since, registers written)
-    for line in lines:
-        op, _, rest = line.partition(" ")
-        operands = [x.strip() for x in rest.split(", ")]
-        if op.startswith("v_mfma"):
-            read = _registers(operands[1]) | _registers(operands[2])
-            found += [line for age, written in recent if age < 2 and read & written]
-        written = set()
-        if op.startswith("v_") and not op.startswith(("v_mfma", "v_cmp", "v_readfirstlane", "v_readlane")):
-            written = _registers(operands[0])
-            if op.startswith(("v_permlane", "v_swap")):
-                written |= _registers(operands[1])
-        step = int(operands[0], 0) + 1 if op == "s_nop" else 1
-        recent = [(age + step, w) for age, w in recent if age + step < 2]
-        if written:
-            recent.append((0, written))
-    return found
-
-
-def test_hazard_finder():
-    write, product = "v_cvt_pk_bf16_f32 v5, v1, v2", "v_mfma_f32_32x32x16_bf16 a[0:15], v[10:13], v[2:5], a[0:15]"
-    assert hazards([write, product]) and hazards([write, "s_waitcnt lgkmcnt(4)", product]) and hazards([write, "s_nop 0", product])
-    assert not hazards([write, "s_nop 1", product]) and not hazards([write, "s_waitcnt vmcnt(0)", "v_xor_b32_e32 v9, 1, v1", product])
-    assert not hazards(["v_cvt_pk_bf16_f32 v6, v1, v2", product]) and hazards(["v_accvgpr_read_b32 v10, a4", product])
-    assert hazards(["v_mov_b32_e32 v13, v2", product]) and not hazards(["v_cmp_gt_i32_e32 vcc, 1, v2", product])
-
-
-def test_products_wait_for_their_operands():
-    lines = codeobj.disassembly(B.LAYER_LIB)
-    assert sum(ln.startswith("v_mfma") for ln in lines) > 200
-    assert hazards(lines) == []
