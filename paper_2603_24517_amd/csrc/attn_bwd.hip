@@ -47,6 +47,7 @@ constexpr int BT = 32;                          // streamed rows per step
 constexpr int TILE_BYTES = BT * ROW_BYTES;      // 8 KiB
 constexpr int ITEM_ROWS = 128;                  // held rows of an item, 32 per wavefront
 constexpr int STATS_BYTES = 2 * BT * 4;         // -LSE and -delta of a step's 32 rows
+constexpr size_t PART_BYTES = 32 * HD * sizeof(float);     // what one wavefront leaves of one sum
 constexpr float LOG2E = 1.4426950408889634f;
 
 // How an item of each kind uses LDS.  While step j runs, the tiles of steps up to j + AHEAD arrive.  Y1 of step j - 1 is still read (in rows items at
@@ -88,13 +89,14 @@ struct Params {
     const __bf16 *q, *k, *v, *dout;
     __bf16 *dq, *dk, *dv;
     const float *stats;
-    float *part_q, *part_kv;        // parts: [split][rows of dq] / [split][dk or dv][rows]
+    unsigned char *part_q, *part_kv;    // parts: [tile][group][piece][wavefront] PART_BYTES each; of keys items twice that, dk and dv
     int B, Hq, Hkv, Sq, Skv, G, qtiles;
     int pack_log2, chunks;          // rows items: query heads of a group side by side, and how many such chunks a group has
     int off;                        // key j valid for row i iff j <= i + off (without the mask: always true)
     float c, scale;                 // c = scale * log2(e)
     Role keys, rows;
-    Div d_hkv, d_chunks;
+    Div d_hkv, d_chunks, d_g;
+    int join_keys;                  // workgroups of attn_bwd_join for dk and dv
 };
 
 // f(0), f(1), ... f(N - 1) with constants (the unroller gives up on a loop of this size)
@@ -207,6 +209,19 @@ __global__ __launch_bounds__(256) void attn_bwd_stats(const __bf16 *dout, const 
 }
 
 // ------------------------------------------------------------------------------------------------------ the products
+// Batch entry, head and first of the 32 rows that a wavefront of an item holds.
+__device__ __forceinline__ void find_rows(const Params &p, bool keys, int group, int tile, int wave, int &b, int &head, int &x0)
+{
+    const int bh = keys ? group : fast_div(group, p.d_chunks);
+    b = fast_div(bh, p.d_hkv);
+    head = bh - b * p.Hkv;
+    x0 = tile * ITEM_ROWS + wave * 32;
+    if (!keys) {
+        head = head * p.G + ((group - bh * p.chunks) << p.pack_log2) + (wave & ((1 << p.pack_log2) - 1));
+        x0 = tile * (ITEM_ROWS >> p.pack_log2) + (wave >> p.pack_log2) * 32;
+    }
+}
+
 // One item: KEYS holds K (X1), V (X2) and streams Q (Y1), dO (Y2); otherwise the reverse.
 template <bool KEYS>
 __device__ __forceinline__ void item(const Params &p, int group, int tile, int piece)
@@ -219,23 +234,9 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
     // ---- what this wavefront holds, and the steps that it streams
-    int b, x_head, x0, x_rows, y_rows, y_head0;
-    if (KEYS) {
-        b = fast_div(group, p.d_hkv);
-        x_head = group - b * p.Hkv;
-        x0 = tile * ITEM_ROWS + wave * 32;
-        x_rows = p.Skv;
-        y_rows = p.Sq;
-        y_head0 = x_head * p.G;
-    } else {
-        const int bh = fast_div(group, p.d_chunks);
-        b = fast_div(bh, p.d_hkv);
-        y_head0 = bh - b * p.Hkv;
-        x_head = y_head0 * p.G + ((group - bh * p.chunks) << p.pack_log2) + (wave & ((1 << p.pack_log2) - 1));
-        x0 = tile * (ITEM_ROWS >> p.pack_log2) + (wave >> p.pack_log2) * 32;
-        x_rows = p.Sq;
-        y_rows = p.Skv;
-    }
+    int b, x_head, x0;
+    find_rows(p, KEYS, group, tile, wave, b, x_head, x0);
+    const int x_rows = KEYS ? p.Skv : p.Sq, y_rows = KEYS ? p.Sq : p.Skv;
     // KEYS: query tiles t0 .. qtiles - 1 of each head; else: key tiles from 0 on
     const int t0 = KEYS ? keys_skip(p, tile) : 0;
     const int per_head = KEYS ? p.qtiles - t0 : rows_steps(p, tile);
@@ -248,7 +249,8 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     }
     // (all of it is wave-uniform: scalar registers)
     auto uniform = [](int &x) __attribute__((always_inline)) { x = __builtin_amdgcn_readfirstlane(x); };
-    uniform(b); uniform(x_head); uniform(x0); uniform(y_head0); uniform(steps);
+    uniform(b); uniform(x_head); uniform(x0); uniform(steps);
+    const int y_head0 = KEYS ? x_head * p.G : fast_div(x_head, p.d_g);
     const int x_heads = KEYS ? p.Hkv : p.Hq, y_heads = KEYS ? p.Hq : p.Hkv;
     const uint32_t y_stride = (uint32_t)y_heads * ROW_BYTES;
 
@@ -347,6 +349,13 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc1[d][r] = acc2[d][r] = 0.0f;
+    auto cleared = [&]() __attribute__((always_inline)) {        // (here, not between the wait for the loads and the first product)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            asm volatile("" : "+v"(acc1[d]));
+            if (KEYS) asm volatile("" : "+v"(acc2[d]));
+        }
+    };
 
     // ---- LDS reads.  Row l32, unit 2 s + hh: as the swizzle is an exclusive or and tiles are 256-byte aligned, that is the address of
     // unit hh with s << 5 flipped.  Transposed: row 4 hh + i / 4 (+ 8 e, + 16 k) and four d's: likewise with d << 6 and e << 5 flipped.
@@ -487,6 +496,7 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
             for (int n = 0; n < PER_STEP; ++n) request_part(n);
             request_done();
         }
+        cleared();
         // (all of them, so that the compiler, which counts the loads above but not these, has none left to wait for in the loop)
         __builtin_amdgcn_s_waitcnt(0);
         wg_barrier();
@@ -514,39 +524,43 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     }
 
     // ---- results: lane = held row, registers 4 d's; exchanged with lane ^ 32, eight in line
+    if (dead) return;
     const int row = x0 + l32;
-    const bool valid = row < x_rows;
-    const size_t at = ((size_t)((size_t)b * x_rows + (valid ? row : 0)) * x_heads + x_head) * HD;
-    auto store = [&](f32x16 (&acc)[4], float f, __bf16 *out, float *part) __attribute__((always_inline)) {
-        if (n_pieces == 1) {
-            unsigned char *op = (unsigned char *)(out + at + 8 * hh);
+    if (n_pieces == 1) {
+        auto store = [&](f32x16 (&acc)[4], float f, __bf16 *out) __attribute__((always_inline)) {
+            u32x4 w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const f32x16 &a = acc[i >> 1];
                 const int e = 8 * (i & 1);
                 auto u = __builtin_amdgcn_permlane32_swap(pack_bf16(a[e] * f, a[e + 1] * f), pack_bf16(a[e + 4] * f, a[e + 5] * f), false, false);
-                auto w = __builtin_amdgcn_permlane32_swap(pack_bf16(a[e + 2] * f, a[e + 3] * f), pack_bf16(a[e + 6] * f, a[e + 7] * f), false, false);
-                const u32x4 ww = {u[0], w[0], u[1], w[1]};
-                if (valid) *(u32x4 *)(op + 32 * i) = ww;
+                auto v = __builtin_amdgcn_permlane32_swap(pack_bf16(a[e + 2] * f, a[e + 3] * f), pack_bf16(a[e + 6] * f, a[e + 7] * f), false, false);
+                w[i] = {u[0], v[0], u[1], v[1]};
             }
-        } else if (valid) {
-            float *op = part + at + 4 * hh;
+            if (row < x_rows) {
+                unsigned char *at = (unsigned char *)(out + ((size_t)((size_t)b * x_rows + row) * x_heads + x_head) * HD + 8 * hh);
 #pragma unroll
-            for (int d = 0; d < 4; ++d)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x16 &a = acc[d];
-                    const f32x4 y = {a[4 * g] * f, a[4 * g + 1] * f, a[4 * g + 2] * f, a[4 * g + 3] * f};
-                    *(f32x4 *)(op + 32 * d + 8 * g) = y;
-                }
-        }
-    };
-    const size_t all = (size_t)p.B * x_rows * x_heads * HD;
-    if (KEYS) {
-        store(acc1, p.scale, p.dk, p.part_kv + (size_t)piece * 2 * all);
-        store(acc2, 1.0f, p.dv, p.part_kv + ((size_t)piece * 2 + 1) * all);
+                for (int i = 0; i < 8; ++i) *(u32x4 *)(at + 32 * i) = w[i];
+            }
+        };
+        store(acc1, p.scale, KEYS ? p.dk : p.dq);
+        if (KEYS) store(acc2, 1.0f, p.dv);
     } else {
-        store(acc1, p.scale, p.dq, p.part_q + (size_t)piece * all);
+        // a part, in the order of the registers: 1 KiB in line at a time
+        unsigned char *at = (KEYS ? p.part_kv : p.part_q) + (((size_t)(tile * (KEYS ? p.keys : p.rows).groups + group) * (KEYS ? p.keys : p.rows).splits + piece) * 4 + wave) *
+                                                                ((KEYS ? 2 : 1) * PART_BYTES) + lane * 16;
+        auto store = [&](f32x16 (&acc)[4], float f) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const f32x16 &a = acc[i >> 2];
+                const int e = 4 * (i & 3);
+                const f32x4 y = {a[e] * f, a[e + 1] * f, a[e + 2] * f, a[e + 3] * f};
+                *(f32x4 *)(at + i * 1024) = y;
+            }
+            at += PART_BYTES;
+        };
+        store(acc1, p.scale);
+        if (KEYS) store(acc2, 1.0f);
     }
 }
 
@@ -581,33 +595,40 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
 }
 
-// The sum of the parts of each tile that was cut, in the order of its pieces: 8 elements per thread, first those of dk and dv, then of dq.
-__global__ __launch_bounds__(256) void attn_bwd_join(const Params p, uint32_t kv_blocks)
+// The sum of the parts of each tile that was cut, in the order of its pieces.  A workgroup adds up one wavefront's 32 rows of one result: 8 elements
+// per thread and pass.
+__global__ __launch_bounds__(256) void attn_bwd_join(const Params p)
 {
-    const bool keys = blockIdx.x < kv_blocks;
-    const int S = keys ? p.Skv : p.Sq, H = keys ? p.Hkv : p.Hq;
-    const size_t all = (size_t)p.B * S * H * HD;
-    const size_t i = ((size_t)(blockIdx.x - (keys ? 0 : kv_blocks)) * 256 + threadIdx.x) * 8;
-    if (i >= all) return;
-    const int pos = (int)((i / HD / H) % S);
-    const int n = keys ? pieces(keys_steps(p, pos / ITEM_ROWS), p.keys.most) : pieces(rows_steps(p, pos / (ITEM_ROWS >> p.pack_log2)), p.rows.most);
-    if (n == 1) return;
-    auto sum = [&](const float *part, size_t stride, __bf16 *out) {
+    const bool keys = (int)blockIdx.x < p.join_keys;
+    const Role &r = keys ? p.keys : p.rows;
+    int n = keys ? blockIdx.x : blockIdx.x - p.join_keys;
+    const int second = keys ? n & 1 : 0;            // dv
+    if (keys) n >>= 1;
+    const int wave = n & 3;
+    n >>= 2;
+    const int tile = n / r.groups, group = n - tile * r.groups;
+    const int count = pieces(keys ? keys_steps(p, tile) : rows_steps(p, tile), r.most);
+    if (count == 1) return;
+    int b, head, x0;
+    find_rows(p, keys, group, tile, wave, b, head, x0);
+    const int rows = keys ? p.Skv : p.Sq, heads = keys ? p.Hkv : p.Hq;
+    const int l32 = threadIdx.x & 31;
+    if (x0 + l32 >= rows) return;
+    const size_t stride = (size_t)4 * (keys ? 2 : 1) * PART_BYTES;
+    const unsigned char *from = (keys ? p.part_kv : p.part_q) + (size_t)(tile * r.groups + group) * r.splits * stride + ((size_t)wave * (keys ? 2 : 1) + second) * PART_BYTES;
+    __bf16 *out = (keys ? second ? p.dv : p.dk : p.dq) + ((size_t)((size_t)b * rows + x0 + l32) * heads + head) * HD;
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass) {
+        const int i = pass * 8 + (threadIdx.x >> 5);        // d = 8 i ..: four from lane l32, four from lane l32 + 32
+        const unsigned char *at = from + i * 1024 + l32 * 16;
         f32x4 a = {0, 0, 0, 0}, c = {0, 0, 0, 0};
 #pragma unroll 4
-        for (int s = 0; s < n; ++s) {
-            const f32x4 *at = (const f32x4 *)(part + (size_t)s * stride + i);
-            a += at[0];
-            c += at[1];
+        for (int s = 0; s < count; ++s, at += stride) {
+            a += *(const f32x4 *)at;
+            c += *(const f32x4 *)(at + 512);
         }
         const u32x4 w = {pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(c[0], c[1]), pack_bf16(c[2], c[3])};
-        *(u32x4 *)(out + i) = w;
-    };
-    if (keys) {
-        sum(p.part_kv, 2 * all, p.dk);
-        sum(p.part_kv + all, 2 * all, p.dv);
-    } else {
-        sum(p.part_q, all, p.dq);
+        *(u32x4 *)(out + 8 * i) = w;
     }
 }
 
@@ -671,6 +692,7 @@ int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &r)
         return ATTN_E_UNSUPPORTED;
     p.d_hkv = make_div(Hkv);
     p.d_chunks = make_div(p.chunks);
+    p.d_g = make_div(G);
     p.keys = {B * Hkv, tk, 1, INT32_MAX};
     p.rows = {B * Hkv * p.chunks, tr, 1, INT32_MAX};
 
@@ -719,8 +741,9 @@ int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &r)
     deal(p.rows);
     auto pad = [](size_t n) { return (n + 255) / 256 * 256; };
     r.stats = pad((size_t)B * Hq * p.qtiles * 2 * BT * sizeof(float));
-    r.part_kv = p.keys.splits > 1 ? pad((size_t)p.keys.splits * 2 * B * Skv * Hkv * HD * sizeof(float)) : 0;
-    r.part_q = p.rows.splits > 1 ? pad((size_t)p.rows.splits * B * Sq * Hq * HD * sizeof(float)) : 0;
+    p.join_keys = p.keys.splits > 1 ? (int)nk * 8 : 0;
+    r.part_kv = p.keys.splits > 1 ? (size_t)p.keys.items * 8 * PART_BYTES : 0;
+    r.part_q = p.rows.splits > 1 ? (size_t)p.rows.items * 4 * PART_BYTES : 0;
     r.total = r.stats + r.part_kv + r.part_q;
     return ATTN_OK;
 }
@@ -776,8 +799,8 @@ int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, 
     p.q = (const __bf16 *)q; p.k = (const __bf16 *)k; p.v = (const __bf16 *)v; p.dout = (const __bf16 *)dout;
     p.dq = (__bf16 *)dq; p.dk = (__bf16 *)dk; p.dv = (__bf16 *)dv;
     p.stats = (const float *)workspace;
-    p.part_kv = (float *)((unsigned char *)workspace + r.stats);
-    p.part_q = (float *)((unsigned char *)workspace + r.stats + r.part_kv);
+    p.part_kv = (unsigned char *)workspace + r.stats;
+    p.part_q = p.part_kv + r.part_kv;
     p.c = scale * LOG2E;
     p.scale = scale;
 
@@ -792,11 +815,9 @@ int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, 
         if (!launch((const void *)attn_bwd_kernel, dim3(p.keys.items + p.rows.items), 256, LDS_BYTES, args, st)) return ATTN_E_LAUNCH;
     }
     if (p.keys.splits > 1 || p.rows.splits > 1) {
-        auto blocks = [](size_t n) { return (uint32_t)((n / 8 + 255) / 256); };
-        uint32_t kv_blocks = p.keys.splits > 1 ? blocks((size_t)B * Skv * Hkv * HD) : 0;
-        const uint32_t q_blocks = p.rows.splits > 1 ? blocks((size_t)B * Sq * Hq * HD) : 0;
-        void *args[] = {&p, &kv_blocks};
-        if (!launch((const void *)attn_bwd_join, dim3(kv_blocks + q_blocks), 256, 0, args, st)) return ATTN_E_LAUNCH;
+        void *args[] = {&p};
+        const int rows = p.rows.splits > 1 ? p.rows.groups * p.rows.tiles * 4 : 0;
+        if (!launch((const void *)attn_bwd_join, dim3(p.join_keys + rows), 256, 0, args, st)) return ATTN_E_LAUNCH;
     }
     return ATTN_OK;
 }
