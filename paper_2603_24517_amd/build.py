@@ -1,7 +1,7 @@
 """Build the gfx950 shared libraries in-tree with hipcc.
 
     python -m paper_2603_24517_amd.build            the attention library (C ABI of include/attn.h), the library of the operators
-                                                     around it (include/attn_layer.h) and the binding's native part
+                                                     around it (include/attn_layer.h) and the binding's native parts
     python -m paper_2603_24517_amd.build --all      that, the measurement-aid library (include/attn_probe.h)
                                                      and every variant of the attention kernel
 
@@ -23,6 +23,8 @@ LAYER_SRCS = [os.path.join(HERE, "csrc", n) for n in ("attn_bwd.hip", "qk_norm_r
 LAYER_LIB = os.path.join(HERE, "libattn_layer_mi355x.so")
 CALL_SRC = os.path.join(HERE, "csrc", "attn_call.cpp")
 CALL_LIB = os.path.join(HERE, "_attn_call.so")
+LAYER_CALL_SRC = os.path.join(HERE, "csrc", "layer_call.cpp")
+LAYER_CALL_LIB = os.path.join(HERE, "_layer_call.so")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -85,19 +87,23 @@ def build_layer(verbose=False):
     return _hipcc([], LAYER_LIB, LAYER_SRCS, verbose)
 
 
-def build_call(verbose=False):
-    """The Python binding's native part: host code against torch's headers and libraries."""
+def build_call(verbose=False, src=CALL_SRC, out=CALL_LIB):
+    """A native part of the Python binding: host code against torch's headers and libraries."""
     import sysconfig
     import torch
     root = os.path.dirname(torch.__file__)
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{root}/include", f"-I{root}/include/torch/csrc/api/include",
-           "-I/opt/rocm/include", f"-I{sysconfig.get_paths()['include']}", "-o", CALL_LIB, CALL_SRC, f"-L{root}/lib", f"-Wl,-rpath,{root}/lib",
+           "-I/opt/rocm/include", f"-I{sysconfig.get_paths()['include']}", "-o", out, src, f"-L{root}/lib", f"-Wl,-rpath,{root}/lib",
            "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip"]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
-    return CALL_LIB
+    return out
+
+
+def build_layer_call(verbose=False):
+    return build_call(verbose, LAYER_CALL_SRC, LAYER_CALL_LIB)
 
 
 def build_variants(names=None, verbose=False):
@@ -109,7 +115,8 @@ def build_all(verbose=False, jobs=4):
     """Everything, a few compilations at a time (each is a single-threaded hipcc run of about ten seconds)."""
     from concurrent.futures import ThreadPoolExecutor
     os.makedirs(VARIANT_DIR, exist_ok=True)
-    tasks = [lambda: build_call(verbose=verbose), lambda: build_layer(verbose=verbose), lambda: build_library(verbose=verbose), lambda: build_probe(verbose=verbose)]
+    tasks = [lambda: build_call(verbose=verbose), lambda: build_layer(verbose=verbose), lambda: build_layer_call(verbose=verbose),
+             lambda: build_library(verbose=verbose), lambda: build_probe(verbose=verbose)]
     tasks += [lambda n=n: build_library(VARIANTS[n], variant_path(n), verbose) for n in VARIANTS]
     with ThreadPoolExecutor(max_workers=jobs) as pool:
         for f in [pool.submit(t) for t in tasks]:
@@ -123,3 +130,4 @@ if __name__ == "__main__":
         print(build_library(extra_flags=sys.argv[1:], verbose=True))
         print(build_layer(verbose=True))
         print(build_call(verbose=True))
+        print(build_layer_call(verbose=True))

@@ -8,6 +8,7 @@ import os
 import paper_2603_24517_amd as _attn
 
 LAYER_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libattn_layer_mi355x.so")
+LAYER_CALL_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_layer_call.so")
 HEAD = 128
 
 ROPE_HALVES, ROPE_ADJACENT = 0, 1
@@ -65,6 +66,28 @@ def attn_bwd(dout, dlse, q, k, v, o, lse, dq, dk, dv, workspace, workspace_bytes
                                  int(bool(causal)), float(scale), stream)
 
 
+class _Native:
+    """csrc/layer_call.cpp, loaded with the first call: attention_backward(), qk_norm_rope() and qk_norm_rope_backward() as one native
+    call each.  None from one of them leaves the call to the general form here, which also words the refusals."""
+
+    def __getattr__(self, name):
+        if not os.path.exists(LAYER_CALL_PATH):
+            raise ImportError(f"{LAYER_CALL_PATH} is missing: build it with `python -m paper_2603_24517_amd.build [--all]`")
+        import importlib.util
+        import torch  # noqa: F401  (its libraries are the module's dependencies)
+        spec = importlib.util.spec_from_file_location(_attn.__name__ + "._layer_call", LAYER_CALL_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        lib = load_layer()
+        module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            lib.attn_bwd, lib.attn_bwd_workspace, lib.attn_qk_norm_rope, lib.attn_qk_norm_rope_bwd, lib.attn_qk_norm_rope_bwd_workspace)))
+        self.backward, self.rope, self.rope_backward = module.backward, module.rope, module.rope_backward
+        return getattr(self, name)
+
+
+_native = _Native()
+
+
 def _on(index):
     """A context in which device `index` is the current one (none where it is already)."""
     import torch
@@ -90,6 +113,16 @@ def attention_backward(do, q, k, v, o, lse, causal=False, scale=None, dlse=None)
     do, q, o [B,Sq,Hq,D], k/v [B,Skv,Hkv,D], BF16; lse, dlse [B,Hq,Sq], FP32; contiguous, on one ROCm device.
     Returns BF16 tensors of the shapes of q, k and v.  Gradients of heads that share K and V are added up.
     """
+    res = _native.backward(do, q, k, v, o, lse, causal, scale, dlse)
+    if type(res) is tuple:
+        return res
+    if res is None:
+        return _attention_backward(do, q, k, v, o, lse, causal, scale, dlse)
+    raise _attn.AttnError(res, "attn_bwd")
+
+
+def _attention_backward(do, q, k, v, o, lse, causal, scale, dlse):
+    """attention_backward() in general: tensor subclasses, torch function modes; and its refusals."""
     import torch
     (B, Sq, Hq, D), (_, Skv, Hkv, _) = _attn._check(q, k, v)
     for t in (do, o):
@@ -198,13 +231,24 @@ def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions=None, eps=1e-6, i
     Returns (q, k), or (q, k, v) with v copied, contiguous as attention() takes them; or writes to the tensors `out`, as many,
     of any strides (a slice of a cache, say), and returns those.
     """
+    if out is not None:
+        out = tuple(out)
+    res = _native.rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, v, out)
+    if type(res) is tuple:
+        return res if out is None else out
+    if res is None:
+        return _qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, v, out)
+    raise _attn.AttnError(res, "attn_qk_norm_rope")
+
+
+def _qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, v, out):
+    """qk_norm_rope() in general."""
     import torch
     rope, index = _rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
     ins = [q, k] if v is None else [q, k, _check_heads("v", v, k.shape, index)]
     if out is None:
         out = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in ins)
     else:
-        out = tuple(out)
         if len(out) != len(ins):
             raise ValueError("out must hold a tensor for each of q, k and (if given) v")
         for t, x in zip(out, ins):
@@ -227,6 +271,18 @@ def qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions=
     or, with dv, (dq, dk, dv, dq_weight, dk_weight): BF16 like the inputs, contiguous or in the tensors `out` (the slices of
     the gradient of one projection, say); the weights' gradients FP32 [D], None without weights.
     """
+    if out is not None:
+        out = tuple(out)
+    res = _native.rope_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, dv, out)
+    if type(res) is tuple:
+        return res if out is None else (*out, *res[-2:])
+    if res is None:
+        return _qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, dv, out)
+    raise _attn.AttnError(res, "attn_qk_norm_rope_bwd")
+
+
+def _qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, dv, out):
+    """qk_norm_rope_backward() in general."""
     import torch
     rope, index = _rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
     grads = [_check_heads("dq", dq, q.shape, index), _check_heads("dk", dk, k.shape, index)]
@@ -235,7 +291,6 @@ def qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions=
     if out is None:
         out = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in grads)
     else:
-        out = tuple(out)
         if len(out) != len(grads):
             raise ValueError("out must hold a tensor for each of dq, dk and (if given) dv")
         for t, x in zip(out, grads):

@@ -351,3 +351,49 @@ def test_norm_rope_in_a_graph_and_on_another_stream():
         other = both()
     torch.cuda.current_stream().wait_stream(side)
     assert all(torch.equal(a, b) for a, b in zip(other, want))
+
+
+# --------------------------------------------------------------------------------------------- native call and general form
+class Sub(torch.Tensor):
+    pass
+
+
+def _equal(a, b):
+    return len(a) == len(b) and all((x is None and y is None) or torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_forms_agree():
+    """The native call, the general form (subclasses, parameters, function modes) and the C entry."""
+    do, q, k, v, o, lse, dl = cuda(*inputs(2, 4, 2, 70, 90, True, seed=6000, dlse=True))
+    ref = A.attention_backward(do, q, k, v, o, lse, True, None, dl)
+    assert type(ref) is tuple
+    assert _equal(A.layer._attention_backward(do, q, k, v, o, lse, True, None, dl), ref)
+    assert _equal(A.attention_backward(do.as_subclass(Sub), q, k, v, o, lse, 1, SCALE, dl), ref)
+    assert _equal(A.attention_backward(do, torch.nn.Parameter(q), k, v, o, lse, causal=True, scale=torch.tensor(SCALE, dtype=torch.float64), dlse=dl), ref)
+    with torch.device("cpu"):
+        assert _equal(A.attention_backward(do, q, k, v, o, lse, True, dlse=dl), ref)
+    nbytes = A.attn_bwd_workspace(2, 4, 2, 70, 90, 128, True)
+    out, ws = [torch.empty_like(t) for t in (q, k, v)], torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    assert A.attn_bwd(do, dl, q, k, v, o, lse, *out, ws, nbytes, 2, 4, 2, 70, 90, 128, True, SCALE, torch.cuda.current_stream().cuda_stream) == 0
+    assert _equal(out, ref)
+
+    case = (2, 30, 6, 2, 96, torch.bfloat16, torch.int32, True, True, True)
+    q, k, v, qw, kw, cos, sin, pos = rope_inputs(*case, seed=6100)
+    q, k, v = on_device(q), on_device(k), on_device(v)
+    qw, kw, cos, sin, pos = cuda(qw, kw, cos, sin, pos)
+    dq, dk, dv = L.rand(6101, *q.shape).cuda(), L.rand(6102, *k.shape).cuda(), L.rand(6103, *v.shape).cuda()
+    args = (qw, kw, cos, sin, pos, 1e-6, True)
+    ref = A.qk_norm_rope(q, k, *args, v=v)
+    assert _equal(A.layer._qk_norm_rope(q, k, *args, v, None), ref)
+    assert _equal(A.qk_norm_rope(q.as_subclass(Sub), k, *args, v=v), ref)
+    assert _equal(A.qk_norm_rope(q, k, torch.nn.Parameter(qw), *args[1:], v), ref)
+    outs = [torch.zeros_like(t) for t in ref]
+    got = A.qk_norm_rope(q, k, *args, v=v, out=outs)
+    assert all(a is b for a, b in zip(got, outs)) and _equal(got, ref)
+    ref = A.qk_norm_rope_backward(dq, dk, q, k, *args, dv=dv)
+    assert _equal(A.layer._qk_norm_rope_backward(dq, dk, q, k, *args, dv, None), ref)
+    with torch.device("cpu"):
+        assert _equal(A.qk_norm_rope_backward(dq, dk, q, k, *args, dv=dv), ref)
+    got = A.qk_norm_rope_backward(dq, dk, q, k, *args, dv=dv, out=outs)
+    assert all(a is b for a, b in zip(got, outs)) and _equal(got, ref)
+    assert _equal(A.qk_norm_rope_backward(dq, dk, q, k, None, None, *args[2:]), A.layer._qk_norm_rope_backward(dq, dk, q, k, None, None, *args[2:], None, None))
