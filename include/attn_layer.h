@@ -39,8 +39,10 @@ extern "C" {
  *   workspace      at least attn_bwd_workspace(...) bytes, 16-byte aligned; contents need not be set and are not kept
  *   B, Hq, Hkv, Sq, Skv, D, causal, scale   as in attn_fwd
  *
- * A value that is not finite may reach the gradients of masked (query, key) pairs of its own tile.
- * Size limits (ATTN_E_UNSUPPORTED): those of attn_fwd; ATTN_E_WORKSPACE if the workspace is too small.
+ * Masked pairs take no part, whatever they hold, but for one thing: a value that is not finite in a row of q or dout, or of k,
+ * makes the gradients of the keys, or queries, that are masked for it but lie within 160 positions of one that is not, NaN.
+ * Size limits (ATTN_E_UNSUPPORTED): those of attn_fwd; B * Hkv * ceil(Skv / 128) and B * Hq * ceil(Sq / 128) below 2^23 and
+ * B * Hq * Sq, with Sq rounded up to a multiple of 32, below 2^30.  ATTN_E_WORKSPACE if the workspace is too small.
  */
 int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, const void *v, const void *o,
              const float *lse, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes,

@@ -163,10 +163,10 @@ __device__ __forceinline__ int swz(int row) { return ((row & 3) << 2) | ((row >>
 // stats[(b * Hq + h) * qtiles + tile][64]: -LSE * log2(e) of the tile's 32 rows, then -delta.  Rows past the end, and rows
 // without a valid key (LSE = -inf), get -inf and 0, so that their P and dS are 0.
 __global__ __launch_bounds__(256) void attn_bwd_stats(const __bf16 *dout, const __bf16 *o, const float *lse, const float *dlse,
-                                                      float *stats, int Hq, int Sq, int qtiles, unsigned rows)
+                                                      float *stats, int Hq, int Sq, int qtiles, unsigned rows, unsigned blocks)
 {
     // 16 lanes per (position, head) row, heads fastest: a wavefront reads 1 KiB in line.  Four rows each, loads first.
-    const unsigned b = blockIdx.y;
+    const unsigned b = blockIdx.x / blocks, block = blockIdx.x - b * blocks;
     const int part = threadIdx.x & 15;
     const size_t base = (size_t)b * Sq * Hq;
     unsigned n[4];
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256) void attn_bwd_stats(const __bf16 *dout, const 
     bool real[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        n[k] = blockIdx.x * 64 + k * 16 + (threadIdx.x >> 4);
+        n[k] = block * 64 + k * 16 + (threadIdx.x >> 4);
         real[k] = n[k] < (unsigned)Sq * (unsigned)Hq;
         const size_t at = (base + (real[k] ? n[k] : 0)) * HD + part * 8;
         x[k] = *(const bf16x8 *)(dout + at);
@@ -688,7 +688,8 @@ int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &r)
     const int pos = ITEM_ROWS >> p.pack_log2;
     const int tk = (Skv + ITEM_ROWS - 1) / ITEM_ROWS, tr = (Sq + pos - 1) / pos;
     const long long nk = (long long)B * Hkv * tk, nr = (long long)B * Hkv * p.chunks * tr;
-    if (nk >= (1ll << 23) || nr >= (1ll << 23) || B > 65535 || (long long)p.qtiles * BT * Hq >= (1ll << 32) - 64 || (long long)p.qtiles * G >= (1ll << 31))
+    // (a launch has fewer than 2^32 threads; each 64 rows of the figures, with 32 of a head in line, take a workgroup of 256)
+    if (nk >= (1ll << 23) || nr >= (1ll << 23) || (long long)p.qtiles * BT * Hq >= (1ll << 30) / B || (long long)p.qtiles * G >= (1ll << 31))
         return ATTN_E_UNSUPPORTED;
     p.d_hkv = make_div(Hkv);
     p.d_chunks = make_div(p.chunks);
@@ -806,9 +807,9 @@ int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, 
 
     {
         float *stats = (float *)workspace;
-        unsigned rows = (unsigned)p.qtiles * BT * (unsigned)Hq;
-        void *args[] = {(void *)&dout, (void *)&o, (void *)&lse, (void *)&dlse, &stats, &Hq, &Sq, &p.qtiles, &rows};
-        if (!launch((const void *)attn_bwd_stats, dim3((rows + 63) / 64, B), 256, 0, args, st)) return ATTN_E_LAUNCH;
+        unsigned rows = (unsigned)p.qtiles * BT * (unsigned)Hq, blocks = rows / 64 + (rows % 64 != 0);
+        void *args[] = {(void *)&dout, (void *)&o, (void *)&lse, (void *)&dlse, &stats, &Hq, &Sq, &p.qtiles, &rows, &blocks};
+        if (!launch((const void *)attn_bwd_stats, dim3(blocks * (unsigned)B), 256, 0, args, st)) return ATTN_E_LAUNCH;
     }
     {
         void *args[] = {&p};

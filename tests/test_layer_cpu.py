@@ -179,3 +179,62 @@ def test_norm_rope_reference_against_differences(interleaved):
             diff = (f(x + e, w) - f(x - e, w)) / (2 * h) if t is x else (f(x, w + e) - f(x, w - e)) / (2 * h)
             assert abs(diff - d.reshape(-1)[i]) < 1e-7
 
+
+
+# ------------------------------------------------------------------------------------------------------- the binding without a device
+def test_exception_of_a_dispatch_mode_reaches_the_caller():
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Refuse(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            if func in (torch.ops.aten.empty_like.default, torch.ops.aten.empty.memory_format):
+                raise KeyError("no")
+            return func(*args, **(kwargs or {}))
+
+    with FakeTensorMode():
+        fake = [torch.empty(1, 4, 2, 128, device="cuda", dtype=torch.bfloat16) for _ in range(5)]
+        lse, cos = torch.empty(1, 2, 4, device="cuda"), torch.empty(4, 64, device="cuda")
+    do, q, k, v, o, lse, cos = (torch._to_functional_tensor(t) for t in (*fake, lse, cos))       # (torch.Tensor itself, on a device)
+    for call in (lambda: A.attention_backward(do, q, k, v, o, lse), lambda: A.qk_norm_rope(q, k, None, None, cos, cos),
+                 lambda: A.qk_norm_rope_backward(do, k, q, k, None, None, cos, cos)):
+        with Refuse(), pytest.raises(KeyError):
+            call()
+
+
+@pytest.mark.parametrize("current", [0, 1])
+def test_device_of_the_tensors_is_made_current_and_its_stream_taken(monkeypatch, current):
+    log = []
+
+    class Context:
+        def __init__(self, index):
+            log.append(("device", index))
+
+        __enter__ = __exit__ = lambda self, *a: None
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current)
+    monkeypatch.setattr(torch.cuda, "device", Context)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 7 + index, raising=False)
+    with layer._on(0):
+        log.append(layer._stream(0))
+    assert log == ([7] if current == 0 else [("device", 0), 7])
+
+
+def test_tensors_of_several_devices_are_refused():
+    class On:
+        def __init__(self, index):
+            self.get_device = lambda: index
+
+    assert layer._same_device([On(1), On(1)]) == 1
+    with pytest.raises(ValueError):
+        layer._same_device([On(0), On(1)])
+
+
+def test_autograd_forms_refuse_what_the_functions_refuse():
+    from paper_2603_24517_amd import autograd as AG
+    x = torch.zeros(1, 8, 4, 128, dtype=torch.bfloat16, requires_grad=True)
+    cos, sin = A.rope_table(8, device="cpu")
+    for call in (lambda: AG.attention(x, x, x), lambda: AG.qk_norm_rope(x, x, None, None, cos, sin), lambda: AG.qkv_norm_rope(x, 2, 1, None, None, cos, sin),
+                 lambda: AG.qkv_norm_rope(x, 2, 2, None, None, cos, sin)):
+        with pytest.raises(ValueError):
+            call()

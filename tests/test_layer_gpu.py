@@ -397,3 +397,74 @@ def test_forms_agree():
     got = A.qk_norm_rope_backward(dq, dk, q, k, *args, dv=dv, out=outs)
     assert all(a is b for a, b in zip(got, outs)) and _equal(got, ref)
     assert _equal(A.qk_norm_rope_backward(dq, dk, q, k, None, None, *args[2:]), A.layer._qk_norm_rope_backward(dq, dk, q, k, None, None, *args[2:], None, None))
+
+
+# ----------------------------------------------------------------------------------------------------------- sizes
+def _device_rand(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda", dtype=torch.bfloat16)
+
+
+def test_backward_of_queries_beyond_32_bit_offsets():
+    """4.6 GB of Q: a few rows with a gradient, the last ones among them, against the same rows alone."""
+    B, Hq, Hkv, Sq, Skv = 1, 128, 2, 140000, 40
+    q, k, v = _device_rand(1, B, Sq, Hq, 128), _device_rand(2, B, Skv, Hkv, 128), _device_rand(3, B, Skv, Hkv, 128)
+    o, lse = A.attention(q, k, v)
+    rows = torch.tensor([0, 1, 70001, 131071, 131072, Sq - 2, Sq - 1], device="cuda")
+    do = torch.zeros_like(q)
+    do[:, rows] = _device_rand(4, B, len(rows), Hq, 128)
+    dq, dk, dv = A.attention_backward(do, q, k, v, o, lse)
+    few = [t[:, rows].cpu() for t in (do, q, o)]
+    want = L.backward64(few[0], few[1], k.cpu(), v.cpu(), few[2], lse[:, :, rows].cpu(), False, SCALE)
+    L.check_backward((dq[:, rows], dk, dv), want)
+    rest = torch.ones(Sq, dtype=torch.bool, device="cuda")
+    rest[rows] = False
+    assert not dq[:, rest].any()
+
+
+def test_backward_of_keys_beyond_32_bit_offsets():
+    B, Hq, Hkv, Sq, Skv = 1, 128, 128, 3, 140000
+    q, do = _device_rand(5, B, Sq, Hq, 128), _device_rand(6, B, Sq, Hq, 128)
+    k, v = _device_rand(7, B, Skv, Hkv, 128), _device_rand(8, B, Skv, Hkv, 128)
+    o, lse = A.attention(q, k, v)
+    dq, dk, dv = A.attention_backward(do, q, k, v, o, lse)
+    keys = torch.tensor([0, 70001, 131071, 131072, Skv - 2, Skv - 1], device="cuda")
+    # these keys alone: LSE and O stay those of all of them
+    ref, bound, _ = L.backward64(do.cpu(), q.cpu(), k[:, keys].cpu(), v[:, keys].cpu(), o.cpu(), lse.cpu(), False, SCALE)
+    for got, n in ((dk[:, keys], 1), (dv[:, keys], 2)):
+        L.check_close(got, (ref[n], bound[n]))
+    for h in (0, 127):      # dq of a head, which is a sum over all keys
+        ref, bound, _ = L.backward64(*(t[:, :, h:h + 1].cpu() for t in (do, q, k, v, o)), lse[:, h:h + 1].cpu(), False, SCALE)
+        L.check_close(dq[:, :, h:h + 1], (ref[0], bound[0]))
+
+
+def test_backward_of_many_short_sequences():
+    B = 70000
+    q, k, v, do = (_device_rand(10 + n, B, 1, h, 128) for n, h in enumerate((2, 1, 1, 2)))
+    o, lse = A.attention(q, k, v, causal=True)
+    dl = torch.randn(B, 2, 1, device="cuda")
+    dq, dk, dv = A.attention_backward(do, q, k, v, o, lse, causal=True, dlse=dl)
+    # one key: P = 1, so dV is the sum of the heads' dO; dS = dLSE, so dQ = scale dLSE K
+    want = do.float().sum(2, keepdim=True)
+    # (P and dS each rounded, the results rounded, P off by 2^-16 before)
+    assert ((dv.float() - want).abs() <= 2.1 * L.H * do.float().abs().sum(2, keepdim=True)).all()
+    want = SCALE * dl.transpose(1, 2)[..., None] * k.float()
+    size = SCALE * (dl.abs().transpose(1, 2)[..., None] + 2 * L.F * (do.float().abs() * v.float().abs()).sum(-1, keepdim=True)) * k.float().abs()
+    assert ((dq.float() - want).abs() <= 2.1 * L.H * size + 2 * L.F * SCALE * (do.float().abs() * v.float().abs()).sum(-1, keepdim=True) * k.float().abs()).all()
+
+
+def test_norm_rope_beyond_32_bit_offsets():
+    S, Hq, Hkv = 70000, 256, 1
+    q, k = _device_rand(20, 1, S, Hq, 128), _device_rand(21, 1, S, Hkv, 128)
+    cos, sin = A.rope_table(S)
+    got = A.qk_norm_rope(q, k, None, None, cos, sin)
+    at = torch.tensor([0, 1, 32767, 65535, 65536, S - 1], device="cuda")
+    places = at.cpu()[None]
+    L.check_close(got[0][:, at], L.norm_rope64(q[:, at].cpu(), None, cos.cpu(), sin.cpu(), places, 1e-6, False))
+    L.check_close(got[1][:, at], L.norm_rope64(k[:, at].cpu(), None, cos.cpu(), sin.cpu(), places, 1e-6, False))
+    w = torch.ones(128, device="cuda")
+    dq = torch.zeros_like(q)
+    dq[:, at] = _device_rand(22, 1, len(at), Hq, 128)
+    dx, _, dqw, _ = A.qk_norm_rope_backward(dq, torch.zeros_like(k), q, k, w, w, cos, sin)
+    (ref, bound), (dw, dw_bound) = L.norm_rope_backward64(dq[:, at].cpu(), q[:, at].cpu(), w.cpu(), cos.cpu(), sin.cpu(), places, 1e-6, False)
+    L.check_close(dx[:, at], (ref, bound))
+    L.check_close(dqw, (dw, dw_bound))
