@@ -50,17 +50,15 @@ constexpr int STATS_BYTES = 2 * BT * 4;         // -LSE and -delta of a step's 3
 constexpr size_t PART_BYTES = 32 * HD * sizeof(float);     // what one wavefront leaves of one sum
 constexpr float LOG2E = 1.4426950408889634f;
 
-// How an item of each kind uses LDS.  While step j runs, the tiles of steps up to j + AHEAD arrive.  Y1 of step j - 1 is still read (in rows items at
-// the end of the step, so that a read of step j - 2's may be on its way when the request that takes its stage leaves); Y2 of step j is read to
-// the end in keys items, to the middle in rows items.  Two workgroups share a compute unit's 160 KiB; keys items, which hold V there, have
-// no room for a stage that covers reads on their way, so a wavefront waits for its reads in front of the barrier.
+// How an item of each kind uses LDS: a ring of stages, each a tile of Y1 and one of Y2 (keys items: and its rows' figures).  While step j runs, step
+// j + 1's tiles arrive.  Keys items read nothing of step j - 1's, and hold V there: two stages, and a wavefront waits for its reads in front of the
+// barrier that hands a stage on.  Rows items still read Y1 of step j - 1, at the end of the step, so that a read of step j - 2's may be on its way
+// when the request that takes its stage leaves: four.  Two workgroups share a compute unit's 160 KiB.
 template <bool KEYS>
 struct Lds {
-    static constexpr int AHEAD = KEYS ? 1 : 2;
     static constexpr bool DRAIN = KEYS;
-    static constexpr int N1 = KEYS ? AHEAD + 2 : AHEAD + 3, N2 = AHEAD + 1, NF = AHEAD + 1;       // stages of Y1, Y2, figures
-    static constexpr int Y2 = N1 * TILE_BYTES, X2 = Y2 + N2 * TILE_BYTES, FIGURES = X2 + (KEYS ? 4 * 32 * ROW_BYTES : 0);
-    static constexpr int BYTES = FIGURES + (KEYS ? NF * STATS_BYTES : 0);
+    static constexpr int STAGES = KEYS ? 2 : 4, X2 = STAGES * 2 * TILE_BYTES, FIGURES = X2 + (KEYS ? 4 * 32 * ROW_BYTES : 0);
+    static constexpr int BYTES = FIGURES + (KEYS ? STAGES * STATS_BYTES : 0);
 };
 constexpr int LDS_BYTES = Lds<true>::BYTES > Lds<false>::BYTES ? Lds<true>::BYTES : Lds<false>::BYTES;
 static_assert(LDS_BYTES <= 80 * 1024);
@@ -94,6 +92,7 @@ struct Params {
     int pack_log2, chunks;          // rows items: query heads of a group side by side, and how many such chunks a group has
     int off;                        // key j valid for row i iff j <= i + off (without the mask: always true)
     float c, scale;                 // c = scale * log2(e)
+    float masked;                   // the score whose probability is 0: c * masked = -inf
     Role keys, rows;
     Div d_hkv, d_chunks, d_g;
     int join_keys;                  // workgroups of attn_bwd_join for dk and dv
@@ -257,21 +256,18 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     // ---- requests: 4 rows x 256 bytes per instruction, two of each tile per wavefront (and, KEYS, a quarter of 256 bytes of figures)
     const int ld_r = lane >> 4, ld_u = lane & 15;
     // Where steps and requests stand: streamed tile, query head of the group, LDS stages; and, for requests, the tiles' addresses.
-    struct At { int tile, head, s1, s2, sf; };
+    struct At { int tile, head, stage; };
     const int y_tiles = KEYS ? p.qtiles : (y_rows + BT - 1) / BT;
     At cur, req;
     cur.head = KEYS && step0 > 0 ? step0 / per_head : 0;
     cur.tile = KEYS ? min(step0 - cur.head * per_head + t0, y_tiles - 1) : min(step0, y_tiles - 1);
     uniform(cur.head);
     uniform(cur.tile);
-    cur.s1 = 0; cur.s2 = L::Y2; cur.sf = L::FIGURES;
+    cur.stage = 0;
     req = cur;
-    auto next1 = [&](int st) __attribute__((always_inline)) { return st == (L::N1 - 1) * TILE_BYTES ? 0 : st + TILE_BYTES; };
-    auto next_stages = [&](At &a) __attribute__((always_inline)) {
-        a.s1 = next1(a.s1);
-        a.s2 = a.s2 == L::Y2 + (L::N2 - 1) * TILE_BYTES ? L::Y2 : a.s2 + TILE_BYTES;
-        if (KEYS) a.sf = a.sf == L::FIGURES + (L::NF - 1) * STATS_BYTES ? L::FIGURES : a.sf + STATS_BYTES;
-    };
+    auto tiles_of = [&](int stage) __attribute__((always_inline)) { return lds0 + stage * (2 * TILE_BYTES); };
+    auto figures_of = [&](int stage) __attribute__((always_inline)) { return lds0 + L::FIGURES + stage * STATS_BYTES; };
+    auto next_stage = [&](int stage) __attribute__((always_inline)) { return (stage + 1) & (L::STAGES - 1); };
     const unsigned char *g1, *g2, *gs = nullptr;
     auto find_tiles = [&]() __attribute__((always_inline)) {
         const size_t at = ((size_t)((size_t)b * y_rows + (size_t)req.tile * BT) * y_heads + y_head0 + req.head) * ROW_BYTES;
@@ -294,15 +290,15 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
         if (n < 4) {
             const int i = n & 1;
             lds_dma16(n < 2 ? g1 : g2, req.tile == y_tiles - 1 ? row_off_last[i] : row_off[i],
-                      __builtin_amdgcn_readfirstlane(lds0 + (n < 2 ? req.s1 : req.s2) + wave * 2048 + i * 1024));
+                      __builtin_amdgcn_readfirstlane(tiles_of(req.stage) + (n < 2 ? 0 : TILE_BYTES) + wave * 2048 + i * 1024));
         } else if (lane < 16) {
-            lds_dma4(gs, (wave * 16 + lane) * 4, __builtin_amdgcn_readfirstlane(lds0 + req.sf + wave * 64));
+            lds_dma4(gs, (wave * 16 + lane) * 4, __builtin_amdgcn_readfirstlane(figures_of(req.stage) + wave * 64));
         }
     };
     // past the end the last step's tiles are read again, into stages that nobody reads, so that the number in flight stays the same
     int left = steps;
     auto request_done = [&]() __attribute__((always_inline)) {
-        next_stages(req);
+        req.stage = next_stage(req.stage);
         if (--left <= 0) return;
         if (KEYS && req.tile == y_tiles - 1) {
             req.tile = t0;
@@ -366,31 +362,31 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
         t_at = row * ROW_BYTES + (((col >> 3) ^ swz(row)) << 4) + (col & 7) * 2;
     }
     typedef const LDS_AS unsigned char *Ptr;
-    auto row_frag = [&](uint32_t tile_at, int s) __attribute__((always_inline)) -> bf16x8 {
-        return *(const LDS_AS bf16x8 *)(Ptr)(uintptr_t)((lds0 + tile_at + r_at) ^ (s << 5));
+    auto row_frag = [&](uint32_t at, int s, int tile) __attribute__((always_inline)) -> bf16x8 {         // `at`: tiles_of() + r_at
+        return *(const LDS_AS bf16x8 *)((Ptr)(uintptr_t)(at ^ (s << 5)) + tile * TILE_BYTES);
     };
-    auto col_frag = [&](uint32_t tile_at, int k, int d) __attribute__((always_inline)) -> bf16x8 {
-        const uint32_t at = (lds0 + tile_at + t_at) ^ (d << 6);
-        s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Ptr)(uintptr_t)at + 16 * k * ROW_BYTES));
-        s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Ptr)(uintptr_t)(at ^ 32) + (16 * k + 8) * ROW_BYTES));
+    auto col_frag = [&](uint32_t at, int k, int d, int tile) __attribute__((always_inline)) -> bf16x8 {    // `at`: tiles_of() + t_at
+        s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Ptr)(uintptr_t)(at ^ (d << 6)) + (tile * TILE_BYTES + 16 * k * ROW_BYTES)));
+        s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)((Ptr)(uintptr_t)(at ^ (d << 6) ^ 32) + (tile * TILE_BYTES + (16 * k + 8) * ROW_BYTES)));
         s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
         return __builtin_bit_cast(bf16x8, v);
     };
 
     // ---- a step: phases of 8 products, each with an operand fragment of Y,
-    //     KEYS:  S(j)   acc1 += Y1^T dS(j-1)   dP(j)   acc2 += Y2^T P(j)
+    //     KEYS:  S(j)   dP(j)   acc2 += Y2^T P(j)   acc1 += Y1^T dS(j)
     //     rows:  S(j)   dP(j)   acc1 += Y1^T dS(j-1)
-    // and between the products the vector work, each piece a phase or two after the products that it needs: rounding dS(j-1) during S(j), the
-    // exponents of S(j) during the two phases after it, P * dP behind dP(j).  Fragments are read LEAD products ahead, across the end of
-    // a step too, so the step's barrier stands LEAD products before its end.
+    // and between the products the vector work, each piece behind the products that it needs and ahead of those that need it: the exponents of S(j)
+    // from dP(j) on, P * dP behind dP(j).  (Rows items have nothing to do between dP(j) and a product with dS(j), so that is a step later.)  Fragments are read
+    // LEAD products ahead, across the end of a step too, so the step's barrier stands LEAD products before its end.
     constexpr int LEAD = 2;
     constexpr int NF = KEYS ? 32 : 24;          // products of a step; fragment f lies in frag[f % 4]
     static_assert(LEAD < 4 && NF % 4 == 0);
-    constexpr int PH_S = 0, PH_DP = KEYS ? 2 : 1, PH_1 = KEYS ? 1 : 2, PH_2 = 3;
-    bf16x8 frag[4], frag2[2];
+    constexpr int PH_S = 0, PH_DP = 1, PH_2 = KEYS ? 2 : -1;
+    bf16x8 frag[4], frag2[4];
     f32x16 s, dp;
     u32x4 pb[2], ds[2];                         // BF16 pairs, the B operands of acc2 and acc1
-    int prev1 = 0;                              // stage of step j - 1's Y1
+    int prev = 0;                               // stage of step j - 1
+    uint32_t r_cur, r_next = tiles_of(0) + r_at, t_cur;
 #pragma unroll
     for (int r = 0; r < 16; ++r) dp[r] = 0.0f;
     // (held in place once four are complete: the compiler otherwise keeps twice as many FP32 values and rounds them right in front of a product)
@@ -401,20 +397,22 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     auto fetch = [&](int f) __attribute__((always_inline)) {
         const int ph = f >> 3, i = f & 7;
         bf16x8 &to = frag[f % 4];
-        if (f >= NF) to = row_frag(next1(cur.s1), i);
-        else if (ph == PH_S) to = row_frag(cur.s1, i);
-        else if (ph == PH_DP) to = row_frag(cur.s2, i);
-        else if (ph == PH_1) to = col_frag(prev1, i >> 2, i & 3);
-        else to = col_frag(cur.s2, i >> 2, i & 3);
+        if (f >= NF) to = row_frag(r_next, i, 0);
+        else if (ph == PH_S) to = row_frag(r_cur, i, 0);
+        else if (ph == PH_DP) to = row_frag(r_cur, i, 1);
+        else to = col_frag(t_cur, i >> 2, i & 3, ph == PH_2 ? 1 : 0);
     };
+    auto fetch2 = [&](int i) __attribute__((always_inline)) { frag2[i & 3] = *(const LDS_AS bf16x8 *)((Ptr)(uintptr_t)(x2_at + lane * 16) + i * 1024); };
     auto step = [&]() __attribute__((always_inline)) {
         const int y0 = cur.tile * BT;
         const bool masked = KEYS ? min(x0 + 32, x_rows) - 1 > y0 + p.off : (y0 + BT - 1 > x0 + p.off || y0 + BT > y_rows);
-        const Ptr figures = (Ptr)(uintptr_t)(lds0 + cur.sf) + 16 * hh;
+        const Ptr figures = (Ptr)(uintptr_t)figures_of(cur.stage) + 16 * hh;
+        r_cur = r_next;
+        t_cur = tiles_of(KEYS ? cur.stage : prev) + t_at;
         f32x4 nlv[4];
         // Masked pairs (KEYS: row < key - off; else key > row + off or key >= Skv) give exactly 0, whatever they hold.  A branch around
         // selects alone: two forms of the whole step meet in copies of hundreds of registers.
-        auto mask = [&](auto &&f) __attribute__((always_inline)) {
+        auto mask = [&](f32x16 &v, float to) __attribute__((always_inline)) {
             if (masked) {
                 int ln = lane;
                 asm volatile("" : "+v"(ln));        // formed here, not kept through all steps
@@ -422,18 +420,21 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int y = 8 * (r >> 2) + (r & 3);
-                    f(r, KEYS ? y >= lim : y <= lim);
+                    v[r] = (KEYS ? y >= lim : y <= lim) ? v[r] : to;
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
         };
         // element e of the vector work
-        auto do_round = [&](int e) __attribute__((always_inline)) { pack(ds, 2 * e, dp[2 * e], dp[2 * e + 1]); };
         auto do_exp = [&](int e) __attribute__((always_inline)) {
             s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], p.c, KEYS ? nlv[e >> 2][e & 3] : nl));
             if (KEYS && (e & 1)) pack(pb, e - 1, s[e - 1], s[e]);
         };
-        auto do_mul = [&](int e) __attribute__((always_inline)) { dp[e] *= s[e]; };
+        auto do_mul = [&](int e) __attribute__((always_inline)) {
+            dp[e] *= s[e];
+            if (KEYS && (e & 1)) pack(ds, e - 1, dp[e - 1], dp[e]);
+        };
+        auto do_round = [&](int e) __attribute__((always_inline)) { pack(ds, 2 * e, dp[2 * e], dp[2 * e + 1]); };
         // the n elements dealt out evenly to `of` slots: those of slot k
         auto spread = [&](int k, int of, int n, auto &&f) __attribute__((always_inline)) {
             if (k < 0 || k >= of) return;
@@ -443,27 +444,24 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
         };
         static_for<NF>([&](auto fc) __attribute__((always_inline)) {
             constexpr int f = decltype(fc)::value, ph = f >> 3, i = f & 7;
-            if constexpr (KEYS && f == 8 * PH_2) {
-                mask([&](int r, bool ok) __attribute__((always_inline)) {
-                    s[r] = ok ? s[r] : 0.0f;
-                    if (r & 1) pack(pb, r - 1, s[r - 1], s[r]);
-                });
-            }
-            if (f == NF - LEAD) {
-                // the next step's tiles have landed (all but those of the steps behind it), for every wavefront
-                __builtin_amdgcn_s_waitcnt(wait_vmcnt((L::AHEAD - 1) * PER_STEP) & (L::DRAIN ? WAIT_LGKMCNT0 : ~0));
+            if constexpr (KEYS && f == 9) mask(s, p.masked);
+            if constexpr (KEYS && f == 17) mask(dp, 0.0f);
+            if constexpr (f == NF - LEAD) {
+                // the next step's tiles have landed, for every wavefront
+                __builtin_amdgcn_s_waitcnt(wait_vmcnt(0) & (L::DRAIN ? WAIT_LGKMCNT0 : ~0));
                 wg_barrier();
+                r_next = tiles_of(next_stage(cur.stage)) + r_at;
             }
             fetch(f + LEAD);
-            if constexpr (KEYS && ((f + 1) >> 3) == PH_DP) frag2[(f + 1) & 1] = *(const LDS_AS bf16x8 *)((Ptr)(uintptr_t)(x2_at + lane * 16) + ((f + 1) & 7) * 1024);
+            if constexpr (KEYS && f >= 6 && f < 14) fetch2(f - 6);
             if (f >= 1 && f <= PER_STEP) request_part(f - 1);
             if (f == PER_STEP + 1) request_done();
             // -LSE, a quarter at a time shortly before its exponents; -delta, where dP starts from
             if constexpr (KEYS && f >= 6 && f < 18 && (f - 6) % 3 == 0) nlv[(f - 6) / 3] = *(const LDS_AS f32x4 *)(figures + 32 * ((f - 6) / 3));
-            if constexpr (KEYS && f >= 8 && f < 12) {
-                const f32x4 d = *(const LDS_AS f32x4 *)(figures + BT * 4 + 32 * (f - 8));
+            if constexpr (KEYS && f >= 3 && f < 7) {
+                const f32x4 d = *(const LDS_AS f32x4 *)(figures + BT * 4 + 32 * (f - 3));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) dp[4 * (f - 8) + e] = d[e];
+                for (int e = 0; e < 4; ++e) dp[4 * (f - 3) + e] = d[e];
             }
             const bf16x8 a = frag[f % 4];
             if constexpr (ph == PH_S) {
@@ -472,30 +470,27 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
                 for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
                 s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, x1[i], i == 0 ? zero : s, 0, 0, 0);
             } else if constexpr (ph == PH_DP) {
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, KEYS ? frag2[i & 1] : x2[i], !KEYS && i == 0 ? nd : dp, 0, 0, 0);
-            } else if constexpr (ph == PH_1) {
-                acc1[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, ds[i >> 2]), acc1[i & 3], 0, 0, 0);
-            } else {
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, KEYS ? frag2[i & 3] : x2[i], !KEYS && i == 0 ? nd : dp, 0, 0, 0);
+            } else if constexpr (ph == PH_2) {
                 acc2[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, pb[i >> 2]), acc2[i & 3], 0, 0, 0);
+            } else {
+                acc1[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, ds[i >> 2]), acc1[i & 3], 0, 0, 0);
             }
-            spread(f, 8, 8, do_round);
-            spread(f - 9, KEYS ? 15 : 11, 16, do_exp);
-            spread(f - (KEYS ? 25 : 17), 7, 16, do_mul);
+            if (!KEYS) spread(f, 8, 8, do_round);
+            spread(f - 9, KEYS ? 10 : 11, 16, do_exp);
+            spread(f - 17, KEYS ? 10 : 7, 16, do_mul);
             __builtin_amdgcn_sched_barrier(0);
         });
-        mask([&](int r, bool ok) __attribute__((always_inline)) { dp[r] = ok ? dp[r] : 0.0f; });
-        prev1 = cur.s1;
-        next_stages(cur);
+        if (!KEYS) mask(dp, 0.0f);
+        prev = cur.stage;
+        cur.stage = next_stage(cur.stage);
         if (KEYS && cur.tile == y_tiles - 1) cur.tile = t0;
         else ++cur.tile;
     };
     if (steps > 0) {
 #pragma unroll
-        for (int i = 0; i < L::AHEAD; ++i) {
-#pragma unroll
-            for (int n = 0; n < PER_STEP; ++n) request_part(n);
-            request_done();
-        }
+        for (int n = 0; n < PER_STEP; ++n) request_part(n);
+        request_done();
         cleared();
         // (all of them, so that the compiler, which counts the loads above but not these, has none left to wait for in the loop)
         __builtin_amdgcn_s_waitcnt(0);
@@ -505,22 +500,23 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
 #pragma unroll
                 for (int n = 0; n < PER_STEP; ++n) request_part(n);
                 request_done();
-                __builtin_amdgcn_s_waitcnt(wait_vmcnt((L::AHEAD - 1) * PER_STEP));
+                __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
                 wg_barrier();
             }
-            __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
             return;
         }
+        r_cur = r_next;
 #pragma unroll
         for (int f = 0; f < LEAD; ++f) fetch(f);
         for (int j = 0; j < steps; ++j) step();
-        __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
-        // the last step's dS
+        if (!KEYS) {            // the last step's dS
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) pack(ds, r, dp[r], dp[r + 1]);
+            for (int r = 0; r < 16; r += 2) pack(ds, r, dp[r], dp[r + 1]);
+            t_cur = tiles_of(prev) + t_at;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            acc1[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag(prev1, i >> 2, i & 3), __builtin_bit_cast(bf16x8, ds[i >> 2]), acc1[i & 3], 0, 0, 0);
+            for (int i = 0; i < 8; ++i)
+                acc1[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag(t_cur, i >> 2, i & 3, 0), __builtin_bit_cast(bf16x8, ds[i >> 2]), acc1[i & 3], 0, 0, 0);
+        }
     }
 
     // ---- results: lane = held row, registers 4 d's; exchanged with lane ^ 32, eight in line
@@ -803,6 +799,8 @@ int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, 
     p.part_kv = (unsigned char *)workspace + r.stats;
     p.part_q = p.part_kv + r.part_kv;
     p.c = scale * LOG2E;
+    if (p.c == 0.0f) p.c = 1.2e-38f;        // (no score is large enough to tell it from 0)
+    p.masked = p.c > 0 ? -INFINITY : INFINITY;
     p.scale = scale;
 
     {
