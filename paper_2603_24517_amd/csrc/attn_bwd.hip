@@ -168,20 +168,25 @@ __global__ __launch_bounds__(256) void attn_bwd_stats(const __bf16 *dout, const 
     const unsigned b = blockIdx.x / blocks, block = blockIdx.x - b * blocks;
     const int part = threadIdx.x & 15;
     const size_t base = (size_t)b * Sq * Hq;
-    unsigned n[4];
+    unsigned n[4], i[4], h[4];
     bf16x8 x[4], y[4];
+    float l[4], dl[4];
     bool real[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         n[k] = block * 64 + k * 16 + (threadIdx.x >> 4);
-        real[k] = n[k] < (unsigned)Sq * (unsigned)Hq;
+        i[k] = n[k] / (unsigned)Hq;
+        h[k] = n[k] - i[k] * Hq;
+        real[k] = i[k] < (unsigned)Sq;
         const size_t at = (base + (real[k] ? n[k] : 0)) * HD + part * 8;
         x[k] = *(const bf16x8 *)(dout + at);
         y[k] = *(const bf16x8 *)(o + at);
+        const size_t figure = real[k] ? ((size_t)b * Hq + h[k]) * Sq + i[k] : 0;
+        l[k] = lse[figure];
+        dl[k] = dlse ? dlse[figure] : 0.0f;
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        if (n[k] >= rows) continue;
         float s = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) s = fmaf((float)x[k][e], (float)y[k][e], s);
@@ -189,20 +194,11 @@ __global__ __launch_bounds__(256) void attn_bwd_stats(const __bf16 *dout, const 
         s += __shfl_xor(s, 2);
         s += __shfl_xor(s, 4);
         s += __shfl_xor(s, 8);
-        const unsigned i = n[k] / (unsigned)Hq, h = n[k] - i * Hq;
-        if (part == 0) {
-            float nl = -INFINITY, nd = 0.0f;
-            if (real[k]) {
-                const size_t at = ((size_t)b * Hq + h) * Sq + i;
-                const float l = lse[at];
-                if (l != -INFINITY) {
-                    nl = -l * LOG2E;
-                    nd = (dlse ? dlse[at] : 0.0f) - s;
-                }
-            }
-            float *out = stats + (((size_t)b * Hq + h) * qtiles + (i >> 5)) * (2 * BT) + (i & 31);
-            out[0] = nl;
-            out[BT] = nd;
+        if (part == 0 && n[k] < rows) {
+            const bool some = real[k] && l[k] != -INFINITY;
+            float *out = stats + (((size_t)b * Hq + h[k]) * qtiles + (i[k] >> 5)) * (2 * BT) + (i[k] & 31);
+            out[0] = some ? -l[k] * LOG2E : -INFINITY;
+            out[BT] = some ? dl[k] - s : 0.0f;
         }
     }
 }

@@ -22,8 +22,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int HD = 128;
 constexpr int LANES = 8;                // per row
-constexpr int UNROLL = 2;               // rows in flight per lane
-constexpr int BLOCK_ROWS = 256 / LANES * UNROLL;
+constexpr int BLOCK_ROWS = 256 / LANES;     // rows of a workgroup at a time.  (Two per lane: 8 x 4096, 48 heads 149 -> 153 us, one token of 64 sequences 2.8 -> 3.5)
 
 // n / d for n < 2^31, found on the host: (umulhi(n, mul) + n) >> shift, or n itself
 struct Div { uint32_t mul, shift; };
@@ -67,6 +66,14 @@ __device__ __forceinline__ float sum8(float x)
     x += __shfl_xor(x, 1);
     x += __shfl_xor(x, 2);
     return x + __shfl_xor(x, 4);
+}
+
+__device__ __forceinline__ float reciprocal_rms(const float (&x)[16], float eps)
+{
+    float q = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) q = fmaf(x[e], x[e], q);
+    return 1.0f / sqrtf(sum8(q) * (1.0f / HD) + eps);
 }
 
 // The 16 elements of lane j: [lo, lo + 8) and [hi, hi + 8); its pairs take table elements 8 j .. 8 j + 7.
@@ -175,16 +182,13 @@ __device__ __forceinline__ bool angles(const Params &p, const Spot &at, int j, b
 __device__ __forceinline__ void copy_rows(const Params &p, const Kind &k, uint32_t first)
 {
     const int j = threadIdx.x & (LANES - 1);
-#pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const Spot at = spot(p, k, first + u * (256 / LANES) + threadIdx.x / LANES);
-        if (!at.real) continue;
-        const bf16x8 *from = (const bf16x8 *)(place(k.x, at.b, at.s, at.h) + 32 * j);
-        bf16x8 *to = (bf16x8 *)(place(k.z, at.b, at.s, at.h) + 32 * j);
-        const bf16x8 a = from[0], c = from[1];
-        to[0] = a;
-        to[1] = c;
-    }
+    const Spot at = spot(p, k, first + threadIdx.x / LANES);
+    if (!at.real) return;
+    const bf16x8 *from = (const bf16x8 *)(place(k.x, at.b, at.s, at.h) + 32 * j);
+    bf16x8 *to = (bf16x8 *)(place(k.z, at.b, at.s, at.h) + 32 * j);
+    const bf16x8 a = from[0], c = from[1];
+    to[0] = a;
+    to[1] = c;
 }
 
 template <bool ADJACENT>
@@ -199,28 +203,16 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const Params p)
         return;
     }
     const Lane<ADJACENT> lane(p.rotated);
-    float x[UNROLL][16], c[UNROLL][8], s[UNROLL][8], w[16];
-    Spot at[UNROLL];
-    bool inside[UNROLL];
-#pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        at[u] = spot(p, k, block * BLOCK_ROWS + u * (256 / LANES) + threadIdx.x / LANES);
-        lane.load(place(k.x, at[u].b, at[u].s, at[u].h), x[u]);
-        inside[u] = angles(p, at[u], lane.j, lane.turns, c[u], s[u]);
-    }
+    float x[16], c[8], s[8], w[16];
+    const Spot at = spot(p, k, block * BLOCK_ROWS + threadIdx.x / LANES);
+    lane.load(place(k.x, at.b, at.s, at.h), x);
+    const bool inside = angles(p, at, lane.j, lane.turns, c, s);
     lane.weights(k.weight, p.wide_weight, w);
+    const float r = inside ? reciprocal_rms(x, p.eps) : NAN;
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        float q = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) q = fmaf(x[u][e], x[u][e], q);
-        float r = 1.0f / sqrtf(sum8(q) * (1.0f / HD) + p.eps);
-        if (!inside[u]) r = NAN;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[u][e] = x[u][e] * r * w[e];
-        lane.template turn<false>(x[u], c[u], s[u]);
-        if (at[u].real) lane.store((unsigned char *)place(k.z, at[u].b, at[u].s, at[u].h), x[u]);
-    }
+    for (int e = 0; e < 16; ++e) x[e] = x[e] * r * w[e];
+    lane.template turn<false>(x, c, s);
+    if (at.real) lane.store((unsigned char *)place(k.z, at.b, at.s, at.h), x);
 }
 
 // The gradient.  Each lane adds up dweight of its 16 elements over its rows; the 32 lanes of a workgroup that hold the same
@@ -244,36 +236,25 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(const Params p)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dw[e] = 0.0f;
     for (uint64_t first = (uint64_t)block * BLOCK_ROWS; first < k.rows; first += stride) {
-        float x[UNROLL][16], z[UNROLL][16], c[UNROLL][8], s[UNROLL][8];
-        Spot at[UNROLL];
-        bool inside[UNROLL];
+        float x[16], z[16], c[8], s[8];
+        const Spot at = spot(p, k, (uint32_t)first + threadIdx.x / LANES);
+        lane.load(place(k.x, at.b, at.s, at.h), x);
+        lane.load(place(k.z, at.b, at.s, at.h), z);
+        const bool inside = angles(p, at, lane.j, lane.turns, c, s);
+        const float r = inside ? reciprocal_rms(x, p.eps) : NAN;
+        lane.template turn<true>(z, c, s);
+        float m = 0.0f;
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            at[u] = spot(p, k, (uint32_t)first + u * (256 / LANES) + threadIdx.x / LANES);
-            lane.load(place(k.x, at[u].b, at[u].s, at[u].h), x[u]);
-            lane.load(place(k.z, at[u].b, at[u].s, at[u].h), z[u]);
-            inside[u] = angles(p, at[u], lane.j, lane.turns, c[u], s[u]);
+        for (int e = 0; e < 16; ++e) {
+            x[e] *= r;                                      // xhat
+            if (at.real) dw[e] = fmaf(z[e], x[e], dw[e]);
+            z[e] *= w[e];
+            m = fmaf(z[e], x[e], m);
         }
+        m = sum8(m) * (1.0f / HD);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            float q = 0.0f, m = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) q = fmaf(x[u][e], x[u][e], q);
-            float r = 1.0f / sqrtf(sum8(q) * (1.0f / HD) + p.eps);
-            if (!inside[u]) r = NAN;
-            lane.template turn<true>(z[u], c[u], s[u]);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                x[u][e] *= r;                                   // xhat
-                if (at[u].real) dw[e] = fmaf(z[u][e], x[u][e], dw[e]);
-                z[u][e] *= w[e];
-                m = fmaf(z[u][e], x[u][e], m);
-            }
-            m = sum8(m) * (1.0f / HD);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) z[u][e] = r * (z[u][e] - x[u][e] * m);
-            if (at[u].real) lane.store((unsigned char *)place(k.dx, at[u].b, at[u].s, at[u].h), z[u]);
-        }
+        for (int e = 0; e < 16; ++e) z[e] = r * (z[e] - x[e] * m);
+        if (at.real) lane.store((unsigned char *)place(k.dx, at.b, at.s, at.h), z);
     }
     if (!p.partial) return;
     float *mine = sums[threadIdx.x / LANES];
@@ -288,26 +269,28 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(const Params p)
     }
 }
 
-// dweight: the workgroups' sums, 16 elements of one weight per workgroup, 16 runs of them side by side.
-__global__ __launch_bounds__(256) void qk_norm_rope_weight_kernel(const float *partial, float *dq_weight, float *dk_weight,
-                                                                  int q_blocks, int k_blocks)
+// dweight: the workgroups' sums, 16 elements of one weight per workgroup, 64 runs of them side by side.
+__global__ __launch_bounds__(1024) void qk_norm_rope_weight_kernel(const float *partial, float *dq_weight, float *dk_weight,
+                                                                   int q_blocks, int k_blocks)
 {
-    __shared__ float sums[16][17];
+    __shared__ float sums[64][17];
     const bool keys = blockIdx.x >= HD / 16;
-    const int e = (blockIdx.x % (HD / 16)) * 16 + (threadIdx.x & 15), run = threadIdx.x >> 4;
+    const int col = threadIdx.x & 15, e = (blockIdx.x % (HD / 16)) * 16 + col, run = threadIdx.x >> 4;
     const float *at = partial + (keys ? (size_t)q_blocks * HD : 0) + e;
     const int n = keys ? k_blocks : q_blocks;
     float t = 0.0f;
-#pragma unroll 8
-    for (int i = run; i < n; i += 16) t += at[(size_t)i * HD];
-    sums[run][threadIdx.x & 15] = t;
+#pragma unroll 16
+    for (int i = run; i < n; i += 64) t += at[(size_t)i * HD];
+    sums[run][col] = t;
     __syncthreads();
-    if (run == 0) {
+    if (run < 4) {
         float a = 0.0f;
 #pragma unroll
-        for (int g = 0; g < 16; ++g) a += sums[g][threadIdx.x];
-        (keys ? dk_weight : dq_weight)[e] = a;
+        for (int g = 0; g < 16; ++g) a += sums[run * 16 + g][col];
+        sums[run * 16][col] = a;        // (its own run's first, which no other run reads)
     }
+    __syncthreads();
+    if (run == 0) (keys ? dk_weight : dq_weight)[e] = (sums[0][col] + sums[16][col]) + (sums[32][col] + sums[48][col]);
 }
 
 // ----------------------------------------------------------------------------------------------------------- host
@@ -315,8 +298,8 @@ constexpr uint32_t MOST_BLOCKS = 1024;      // backward, of one kind: what fills
 
 uint32_t bwd_blocks(uint32_t rows)
 {
-    const uint32_t n = (rows + BLOCK_ROWS - 1) / BLOCK_ROWS;
-    return n < MOST_BLOCKS ? n : MOST_BLOCKS;
+    const uint32_t n = (rows + BLOCK_ROWS - 1) / BLOCK_ROWS, each = (n + MOST_BLOCKS - 1) / MOST_BLOCKS;
+    return n == 0 ? 0 : (n + each - 1) / each;
 }
 int check_rope(const attn_rope *r)
 {
@@ -370,9 +353,9 @@ void fill(const attn_rope *r, bool values, Params &p)
     p.wide_weight = r->weight_type == ATTN_FP32;
     p.eps = r->eps;
 }
-bool launch(const void *kernel, unsigned grid, void **args, hipStream_t st)
+bool launch(const void *kernel, unsigned grid, void **args, hipStream_t st, int threads = 256)
 {
-    if (hipLaunchKernel(kernel, dim3(grid), dim3(256), args, 0, st) == hipSuccess) return true;
+    if (hipLaunchKernel(kernel, dim3(grid), dim3(threads), args, 0, st) == hipSuccess) return true;
     (void)hipGetLastError();
     return false;
 }
@@ -438,7 +421,7 @@ int attn_qk_norm_rope_bwd(const attn_rope *r, const attn_heads *dq_out, const at
     if (dq_weight) {
         int nq = p.kind[0].blocks, nk = p.kind[1].blocks;
         void *sum[] = {&p.partial, &dq_weight, &dk_weight, &nq, &nk};
-        if (!launch((const void *)qk_norm_rope_weight_kernel, 2 * (HD / 16), sum, st)) return ATTN_E_LAUNCH;
+        if (!launch((const void *)qk_norm_rope_weight_kernel, 2 * (HD / 16), sum, st, 1024)) return ATTN_E_LAUNCH;
     }
     return ATTN_OK;
 }
