@@ -9,6 +9,7 @@
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -65,16 +66,19 @@ int size(int64_t n)
 bool on(const at::Tensor &t, const at::Tensor &q) { return !t.defined() || (t.is_cuda() && t.device() == q.device()); }
 void *ptr(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
 
-// f(stream), without the interpreter's lock, with q's device current
+// f(stream, workspace), without the interpreter's lock, with q's device current.  The workspace, if any, comes from torch's allocator, as a tensor's
+// memory would: it belongs to the stream, and goes back to it when the call has been enqueued.
 template <class F>
-int launch(const at::Tensor &q, F &&f)
+int launch(const at::Tensor &q, long long bytes, F &&f)
 {
     const auto index = q.get_device();
-    void *stream = (void *)c10::hip::getCurrentHIPStream(index).stream();
     int rc;
     auto go = [&]() {
+        void *stream = (void *)c10::hip::getCurrentHIPStream(index).stream();
+        c10::DataPtr workspace;
+        if (bytes > 0) workspace = c10::hip::HIPCachingAllocator::get()->allocate((size_t)bytes);
         Py_BEGIN_ALLOW_THREADS
-        rc = f(stream);
+        rc = f(stream, workspace.get());
         Py_END_ALLOW_THREADS
     };
     if (index == c10::hip::current_device()) {
@@ -143,10 +147,10 @@ PyObject *backward(PyObject *, PyObject *const *args, Py_ssize_t n)
         const float scale = (float)(args[7] == Py_None ? std::pow((double)D, -0.5) : number(args[7]));
         const long long bytes = bwd_workspace(B, Hq, Hkv, Sq, Skv, D, causal);
         if (bytes < 0) return PyLong_FromLongLong(bytes);
-        const at::Tensor dq = at::empty_like(q), dk = at::empty_like(k), dv = at::empty_like(v), workspace = at::empty({bytes}, q.options().dtype(at::kByte));
-        const int rc = launch(q, [&](void *stream) {
+        const at::Tensor dq = at::empty_like(q), dk = at::empty_like(k), dv = at::empty_like(v);
+        const int rc = launch(q, bytes, [&](void *stream, void *workspace) {
             return bwd(ptr(dout), (const float *)ptr(dlse), ptr(q), ptr(k), ptr(v), ptr(o), (const float *)ptr(lse), ptr(dq), ptr(dk), ptr(dv),
-                       ptr(workspace), (size_t)bytes, B, Hq, Hkv, Sq, Skv, D, causal, scale, stream);
+                       workspace, (size_t)bytes, B, Hq, Hkv, Sq, Skv, D, causal, scale, stream);
         });
         return rc != 0 ? PyLong_FromLong(rc) : tuple({dq, dk, dv});
     });
@@ -250,7 +254,7 @@ PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t n)
             h[i] = heads(in[i]);
             h[3 + i] = heads(out[i]);
         }
-        const int rc = launch(x.q, [&](void *stream) { return rope_fwd(&x.r, h, h + 1, h + 2, h + 3, h + 4, h + 5, stream); });
+        const int rc = launch(x.q, 0, [&](void *stream, void *) { return rope_fwd(&x.r, h, h + 1, h + 2, h + 3, h + 4, h + 5, stream); });
         return rc != 0 ? PyLong_FromLong(rc) : tuple(out);
     });
 }
@@ -268,13 +272,12 @@ PyObject *rope_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
             in.push_back(dv);
         }
         std::vector<at::Tensor> out = results(args[12], in);
-        at::Tensor dw[2], workspace;
+        at::Tensor dw[2];
         long long bytes = 0;
         if (x.qw.defined()) {
             bytes = rope_workspace(&x.r);
             if (bytes < 0) return PyLong_FromLongLong(bytes);
             for (at::Tensor &w : dw) w = at::empty({x.r.D}, x.q.options().dtype(at::kFloat));
-            workspace = at::empty({bytes}, x.q.options().dtype(at::kByte));
         }
         attn_heads h[8] = {};
         for (size_t i = 0; i < in.size(); ++i) {
@@ -283,8 +286,8 @@ PyObject *rope_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
         }
         h[3] = heads(x.q);
         h[4] = heads(x.k);
-        const int rc = launch(x.q, [&](void *stream) {
-            return rope_bwd(&x.r, h, h + 1, h + 2, h + 3, h + 4, h + 5, h + 6, h + 7, (float *)ptr(dw[0]), (float *)ptr(dw[1]), ptr(workspace), (size_t)bytes, stream);
+        const int rc = launch(x.q, bytes, [&](void *stream, void *workspace) {
+            return rope_bwd(&x.r, h, h + 1, h + 2, h + 3, h + 4, h + 5, h + 6, h + 7, (float *)ptr(dw[0]), (float *)ptr(dw[1]), workspace, (size_t)bytes, stream);
         });
         if (rc != 0) return PyLong_FromLong(rc);
         out.push_back(dw[0]);
