@@ -515,24 +515,31 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
         }
     }
 
-    // ---- results: lane = held row, registers 4 d's; exchanged with lane ^ 32, eight in line
+    // ---- results: lane = held row, registers 4 d's; exchanged with lane ^ 32, eight in line, and through LDS into whole rows
     if (dead) return;
-    const int row = x0 + l32;
     if (n_pieces == 1) {
+        if (!KEYS) wg_barrier();        // (keys items: where the wavefront's V was; rows items: stages that every wavefront is done with)
+        const uint32_t rows_at = KEYS ? x2_at : lds0 + wave * (32 * ROW_BYTES);
         auto store = [&](f32x16 (&acc)[4], float f, __bf16 *out) __attribute__((always_inline)) {
-            u32x4 w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const f32x16 &a = acc[i >> 1];
                 const int e = 8 * (i & 1);
                 auto u = __builtin_amdgcn_permlane32_swap(pack_bf16(a[e] * f, a[e + 1] * f), pack_bf16(a[e + 4] * f, a[e + 5] * f), false, false);
                 auto v = __builtin_amdgcn_permlane32_swap(pack_bf16(a[e + 2] * f, a[e + 3] * f), pack_bf16(a[e + 6] * f, a[e + 7] * f), false, false);
-                w[i] = {u[0], v[0], u[1], v[1]};
+                const u32x4 w = {u[0], v[0], u[1], v[1]};
+                *(LDS_AS u32x4 *)(uintptr_t)(rows_at + l32 * ROW_BYTES + (((2 * i + hh) ^ (l32 & 15)) << 4)) = w;
             }
-            if (row < x_rows) {
-                unsigned char *at = (unsigned char *)(out + ((size_t)((size_t)b * x_rows + row) * x_heads + x_head) * HD + 8 * hh);
+            u32x4 w[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) *(u32x4 *)(at + 32 * i) = w[i];
+            for (int i = 0; i < 8; ++i) {
+                const int row = 4 * i + ld_r;
+                w[i] = *(const LDS_AS u32x4 *)(uintptr_t)(rows_at + row * ROW_BYTES + ((ld_u ^ (row & 15)) << 4));
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int row = x0 + 4 * i + ld_r;
+                if (row < x_rows) *(u32x4 *)(out + ((size_t)((size_t)b * x_rows + row) * x_heads + x_head) * HD + 8 * ld_u) = w[i];
             }
         };
         store(acc1, p.scale, KEYS ? p.dk : p.dq);
