@@ -13,11 +13,20 @@
 //   * a "keys" item holds K and V of 128 keys and streams Q and dO of every query head that shares them;
 //   * a "rows" item holds Q and dO of 128 query rows and streams K and V.
 // Both are the same loop with the operands' names exchanged.  X1, X2 stand for what is held, Y1, Y2 for what streams:
-//     S = Y1 X1^T     dP = Y2 X2^T - delta     acc1 += Y1^T dS     (keys only) acc2 += Y2^T P
+//     S = Y1 X1^T     dP = Y2 X2^T - delta     (keys only) acc2 += Y2^T P     acc1 += Y1^T dS
 // With v_mfma_f32_32x32x16_bf16 and Y as the A operand, the accumulator layout puts one held row (lane % 32) in each lane
 // and 16 of the tile's 32 streamed rows in its registers, so P and dS are, packed to BF16 in registers, directly the B operands of the
 // products with Y^T, which the transposing read ds_read_b64_tr_b16 fetches from the same tile in LDS: nothing
 // of size rows x keys leaves the registers.
+//
+// What bounds it: 14 * 128 FLOP per pair of unmasked row and key on the matrix pipe.  8 x 4096, 16 heads: 3.15 ms, 1.22 PFLOP/s of products (a library
+// product of 8192^3 on the same card 1.26), the pipe 75 % busy at the 1.53 GHz that the board's power leaves; memory reads and writes are
+// 0.2 ms of it.  A wavefront holds 32 rows, a workgroup is four of them, and two workgroups share a compute unit: one's vector
+// instructions, LDS latencies, first loads and results pass behind the other's products.  The step's order and the place of every vector instruction in it
+// are fixed by hand (sched_barrier), because the registers, 256 per wavefront of which sums and held operands take 160, leave no room for the
+// order that the compiler picks.  Holding 64 rows per wavefront, one workgroup per unit (512 registers, half the LDS reads), was 4 % faster for the largest calls
+// and up to a third slower for small ones, as nothing fills its waits; with two forms of the step, masked or not, the compiler copied up to 300
+// registers where they meet.
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -291,7 +300,8 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
             lds_dma4(gs, (wave * 16 + lane) * 4, __builtin_amdgcn_readfirstlane(figures_of(req.stage) + wave * 64));
         }
     };
-    // past the end the last step's tiles are read again, into stages that nobody reads, so that the number in flight stays the same
+    // past the end the last step's tiles are read again, into a stage that nobody reads (to ask in every step whether there is one more took
+    // 1 % longer, 8 x 4096, and gained nothing for 24 x 200)
     int left = steps;
     auto request_done = [&]() __attribute__((always_inline)) {
         req.stage = next_stage(req.stage);
