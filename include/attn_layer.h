@@ -85,6 +85,8 @@ typedef struct {
  * with cos and sin of the token's table row; computed in FP32, rounded to BF16 once.  v, where given (v_in->ptr not NULL), is
  * copied, so that slices of one projection come out as the contiguous tensors that attn_fwd takes, in one pass.
  * A token whose place lies outside the table gets NaN in q and k.
+ * Size limits (ATTN_E_UNSUPPORTED), for both directions: B * S * Hq and B * S * Hkv at most 2^31 - 2^16; here also the heads of all tokens,
+ * B * S * (Hq + Hkv), or B * S * (Hq + 2 * Hkv) with v, below 2^29 - 96.
  */
 int attn_qk_norm_rope(const attn_rope *r, const attn_heads *q_in, const attn_heads *k_in, const attn_heads *v_in,
                       const attn_heads *q_out, const attn_heads *k_out, const attn_heads *v_out, void *stream);

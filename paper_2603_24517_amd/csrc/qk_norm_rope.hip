@@ -378,6 +378,7 @@ int attn_qk_norm_rope(const attn_rope *r, const attn_heads *q_in, const attn_hea
     if (given(v_in) && ((rc = take_tensor(v_in, r, r->Hkv, p.kind[2].x)) || (rc = take_tensor(v_out, r, r->Hkv, p.kind[2].z)))) return rc;
     unsigned blocks = 0;
     for (Kind &k : p.kind) blocks += k.blocks = (k.rows + BLOCK_ROWS - 1) / BLOCK_ROWS;
+    if (blocks >= 1u << 24) return ATTN_E_UNSUPPORTED;      // (a launch has fewer than 2^32 threads)
     void *args[] = {&p};
     const void *kernel = r->pairing == ATTN_ROPE_ADJACENT ? (const void *)qk_norm_rope_kernel<true> : (const void *)qk_norm_rope_kernel<false>;
     return launch(kernel, blocks, args, (hipStream_t)stream) ? ATTN_OK : ATTN_E_LAUNCH;

@@ -102,6 +102,12 @@ def test_norm_rope_refuses_tensors(backward):
     assert optional[0] == 2
 
 
+def test_norm_rope_refuses_more_rows_than_a_launch_takes():
+    sizes = dict(B=1 << 12, S=1 << 12, places=1 << 12, Hkv=8)
+    assert _rope_call(False, dict(sizes, Hq=16)) == A.ATTN_E_UNSUPPORTED
+    assert _rope_call(False, dict(sizes, Hq=24), {2: layer.Heads(None, 0, 0, 0)}) == A.ATTN_E_UNSUPPORTED
+
+
 def test_norm_rope_backward_refuses_its_own():
     for extra, code in (((4096, None, 12288, 1 << 20), A.ATTN_E_NULL), ((4096, 8192, None, 1 << 20), A.ATTN_E_NULL),
                         ((4096, 8192, 12288, 100), A.ATTN_E_WORKSPACE), ((4097, 8192, 12288, 1 << 20), A.ATTN_E_ALIGN),
