@@ -29,7 +29,7 @@ class _Attention(torch.autograd.Function):
         if do is None and dlse is None:
             return None, None, None, None, None
         q, k, v, o, lse = ctx.saved_tensors
-        do = torch.zeros_like(q) if do is None else do.contiguous()
+        do = torch.zeros_like(q) if do is None else _whole(do)
         dlse = None if dlse is None else dlse.contiguous()
         return (*_attn.attention_backward(do, q, k, v, o, lse, ctx.causal, ctx.scale, dlse), None, None)
 
@@ -82,10 +82,15 @@ class _FusedNormRope(torch.autograd.Function):
         return dqkv, None, None, _as(dqw, q_weight), _as(dkw, k_weight), None, None, None, None, None
 
 
+def _whole(g):
+    """A contiguous gradient on a 16-byte boundary (a view into a larger one may be contiguous and off it)."""
+    return g.contiguous() if not g.is_contiguous() else g if g.data_ptr() % 16 == 0 else g.clone()
+
+
 def _last(g):
     """A gradient with strides that the kernels take: its last dimension contiguous, the others multiples of 8 elements, from 16 bytes on."""
     ok = g.stride(3) == 1 and all(n == 1 or s % 8 == 0 for n, s in zip(g.shape[:3], g.stride())) and g.data_ptr() % 16 == 0
-    return g if ok else g.contiguous() if not g.is_contiguous() else g.clone()
+    return g if ok else _whole(g)
 
 
 def _as(gradient, weight):

@@ -68,6 +68,21 @@ def test_separate_projections_and_strided_gradients():
     assert torch.equal(torch.autograd.grad(none, v)[0], torch.ones_like(v))
 
 
+def test_gradients_off_a_16_byte_boundary():
+    B, S, H = 1, 20, 2
+    q, k, v = (leaf(L.rand(17 + n, B, S, H, 128)) for n in range(3))
+    cos, sin = (t.cuda() for t in L.table(S, 128))
+    odd = lambda seed: torch.cat([torch.zeros(1, dtype=torch.bfloat16), L.rand(seed, B * S * H * 128)]).cuda()[1:].view(B, S, H, 128)
+    do, dk = odd(20), odd(21)
+    assert do.is_contiguous() and do.data_ptr() % 16
+    for f in (lambda: AG.attention(q, k, v, True)[:1], lambda: AG.qk_norm_rope(q, k, None, None, cos, sin)):
+        out = f()
+        got = torch.autograd.grad(out, (q, k), (do, dk)[:len(out)])
+        out = f()
+        want = torch.autograd.grad(out, (q, k), (do.clone(), dk.clone())[:len(out)])
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_attention_gradients_of_one_result_only():
     q, k, v = leaf(L.rand(21, 1, 50, 4, 128)), leaf(L.rand(22, 1, 60, 2, 128)), leaf(L.rand(23, 1, 60, 2, 128))
     o, lse = A.attention(q.detach(), k.detach(), v.detach(), causal=True)
