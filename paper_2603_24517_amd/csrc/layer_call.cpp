@@ -234,8 +234,17 @@ std::vector<at::Tensor> results(PyObject *out, const std::vector<at::Tensor> &li
         all.push_back(tensor(PyTuple_GET_ITEM(out, (Py_ssize_t)i)));
         check_heads(all.back(), like[i]);
         check_output(all.back());
+        for (size_t j = 0; j < i; ++j) require(all[j].data_ptr() != all[i].data_ptr());
     }
     return all;
+}
+
+// The caller's tensors have been written to: autograd counts that, so that a graph that saved one does not take the new values for the old.
+void written(PyObject *out, const std::vector<at::Tensor> &all)
+{
+    if (out == Py_None) return;
+    for (const at::Tensor &t : all)
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
 
 // rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved, v, out)
@@ -255,7 +264,9 @@ PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t n)
             h[3 + i] = heads(out[i]);
         }
         const int rc = launch(x.q, 0, [&](void *stream, void *) { return rope_fwd(&x.r, h, h + 1, h + 2, h + 3, h + 4, h + 5, stream); });
-        return rc != 0 ? PyLong_FromLong(rc) : tuple(out);
+        if (rc != 0) return PyLong_FromLong(rc);
+        written(args[10], out);
+        return tuple(out);
     });
 }
 
@@ -290,6 +301,7 @@ PyObject *rope_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
             return rope_bwd(&x.r, h, h + 1, h + 2, h + 3, h + 4, h + 5, h + 6, h + 7, (float *)ptr(dw[0]), (float *)ptr(dw[1]), workspace, (size_t)bytes, stream);
         });
         if (rc != 0) return PyLong_FromLong(rc);
+        written(args[12], out);
         out.push_back(dw[0]);
         out.push_back(dw[1]);
         return tuple(out);

@@ -185,6 +185,18 @@ def _check_out(out):
     return out
 
 
+def _check_distinct(out):
+    if len({t.data_ptr() for t in out}) < len(out):
+        raise ValueError("outputs must not share memory")
+
+
+def _written(out):
+    """Autograd's counts of the tensors, which the kernels write to behind its back."""
+    from torch.autograd.graph import increment_version
+    for t in out:
+        increment_version(t)
+
+
 def _rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved):
     """(attn_rope, device index) of the arguments that both directions share."""
     import torch
@@ -229,7 +241,7 @@ def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions=None, eps=1e-6, i
     (2 i, 2 i + 1), otherwise (i, i + rotated / 2).
 
     Returns (q, k), or (q, k, v) with v copied, contiguous as attention() takes them; or writes to the tensors `out`, as many,
-    of any strides (a slice of a cache, say), and returns those.
+    of any strides (a slice of a cache, say), and returns those.  They must not share memory with each other or with the inputs.
     """
     if out is not None:
         out = tuple(out)
@@ -254,12 +266,14 @@ def _qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleave
         for t, x in zip(out, ins):
             _check_heads("out", t, x.shape, index)
         _check_out(out)
+        _check_distinct(out)
     null = Heads(None, 0, 0, 0)
     args = [_heads(t) for t in ins] + [null] * (3 - len(ins)) + [_heads(t) for t in out] + [null] * (3 - len(ins))
     with _on(index):
         rc = load_layer().attn_qk_norm_rope(rope, *args, _stream(index))
     if rc != _attn.ATTN_OK:
         raise _attn.AttnError(rc, "attn_qk_norm_rope")
+    _written(out)
     return out
 
 
@@ -269,7 +283,8 @@ def qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions=
 
     Arguments as there; dq, dk, dv: BF16, of the shapes of q and k, last dimension contiguous.  Returns (dq, dk, dq_weight, dk_weight)
     or, with dv, (dq, dk, dv, dq_weight, dk_weight): BF16 like the inputs, contiguous or in the tensors `out` (the slices of
-    the gradient of one projection, say); the weights' gradients FP32 [D], None without weights.
+    the gradient of one projection, say), which must not share memory with each other or with the inputs; the weights' gradients
+    FP32 [D], None without weights.
     """
     if out is not None:
         out = tuple(out)
@@ -296,6 +311,7 @@ def _qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions
         for t, x in zip(out, grads):
             _check_heads("out", t, x.shape, index)
         _check_out(out)
+        _check_distinct(out)
     lib = load_layer()
     dqw = dkw = workspace = None
     nbytes = 0
@@ -313,4 +329,5 @@ def _qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions
         rc = lib.attn_qk_norm_rope_bwd(rope, *args, ptr(dqw), ptr(dkw), ptr(workspace), nbytes, _stream(index))
     if rc != _attn.ATTN_OK:
         raise _attn.AttnError(rc, "attn_qk_norm_rope_bwd")
+    _written(out)
     return (*out, dqw, dkw)

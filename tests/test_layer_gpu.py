@@ -353,6 +353,31 @@ def test_norm_rope_in_a_graph_and_on_another_stream():
     assert all(torch.equal(a, b) for a, b in zip(other, want))
 
 
+def test_norm_rope_out_counts_as_written():
+    """Tensors given as `out` were written to: an autograd graph that saved one says so; and the same one twice is refused."""
+    q, k = L.rand(5200, 1, 4, 2, 128).cuda(), L.rand(5201, 1, 4, 2, 128).cuda()
+    cos, sin = cuda(*L.table(4, 128))
+    args = (None, None, cos, sin)
+    forward = lambda out: A.qk_norm_rope(q, k, *args, out=out)
+    backward = lambda out: A.qk_norm_rope_backward(q, k, q, k, *args, out=out)
+    general = (lambda out: A.layer._qk_norm_rope(q, k, *args, None, 1e-6, False, None, out),
+               lambda out: A.layer._qk_norm_rope_backward(q, k, q, k, *args, None, 1e-6, False, None, out))
+    for call in (forward, backward, *general):
+        out = (torch.zeros_like(q), torch.zeros_like(k))
+        x = torch.ones_like(q).requires_grad_()
+        product = (x * out[1]).sum()
+        call(out)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            product.backward()
+        with torch.inference_mode():
+            made_here = (torch.empty_like(q), torch.empty_like(k))
+            call(made_here)
+        assert _equal(made_here, out)
+        call(made_here)
+        with pytest.raises(ValueError):
+            call((out[0], out[0]))
+
+
 # --------------------------------------------------------------------------------------------- native call and general form
 class Sub(torch.Tensor):
     pass
