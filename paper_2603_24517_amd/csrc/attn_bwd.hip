@@ -20,8 +20,8 @@
 // of size rows x keys leaves the registers.
 //
 // What bounds it: 14 * 128 FLOP per pair of unmasked row and key on the matrix pipe.  8 x 4096, 16 heads: 3.15 ms, 1.22 PFLOP/s of products (a library
-// product of 8192^3 on the same card 1.26), the pipe 75 % busy at the 1.53 GHz that the board's power leaves; memory reads and writes are
-// 0.2 ms of it.  A wavefront holds 32 rows, a workgroup is four of them, and two workgroups share a compute unit: one's vector
+// product of 8192^3 on the same card 1.24), the pipe 74 % busy at the 1.56 GHz that the board's power leaves; memory reads and writes are
+// 0.4 ms of it.  A wavefront holds 32 rows, a workgroup is four of them, and two workgroups share a compute unit: one's vector
 // instructions, LDS latencies, first loads and results pass behind the other's products.  The step's order and the place of every vector instruction in it
 // are fixed by hand (sched_barrier), because the registers, 256 per wavefront of which sums and held operands take 160, leave no room for the
 // order that the compiler picks.  Holding 64 rows per wavefront, one workgroup per unit (512 registers, half the LDS reads), was 4 % faster for the largest calls

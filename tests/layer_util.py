@@ -125,7 +125,7 @@ def norm_rope64(x, w, cos, sin, positions, eps, interleaved):
 
 def norm_rope_backward64(dz, x, w, cos, sin, positions, eps, interleaved):
     """((dx, bound), (dweight, bound)).  A weight's gradient is a sum in FP32 of up to a few hundred terms in line per lane, then of 32 lanes,
-    1024 workgroups in 16 runs: 2^-24 * 2^9 of the sum of magnitudes."""
+    then of 1024 workgroups in 64 runs: 2^-24 * 2^9 of the sum of magnitudes."""
     x = x.double()
     r = 1.0 / torch.sqrt((x * x).mean(-1, keepdim=True) + eps)
     xhat = x * r
