@@ -8,7 +8,9 @@
 
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -65,6 +67,13 @@ int size(int64_t n)
 }
 bool on(const at::Tensor &t, const at::Tensor &q) { return !t.defined() || (t.is_cuda() && t.device() == q.device()); }
 void *ptr(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// A fresh contiguous tensor on q's device.  No dispatch mode wants to see it: past torch's dispatcher, which takes longer than the allocation.
+at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor &q)
+{
+    if (c10::impl::TorchDispatchModeTLS::any_modes_set()) return at::empty(sizes, q.options().dtype(type));
+    return at::Tensor(at::detail::empty_cuda(sizes, type, q.device(), std::nullopt));
+}
 
 // f(stream, workspace), without the interpreter's lock, with q's device current.  The workspace, if any, comes from torch's allocator, as a tensor's
 // memory would: it belongs to the stream, and goes back to it when the call has been enqueued.
@@ -147,7 +156,7 @@ PyObject *backward(PyObject *, PyObject *const *args, Py_ssize_t n)
         const float scale = (float)(args[7] == Py_None ? std::pow((double)D, -0.5) : number(args[7]));
         const long long bytes = bwd_workspace(B, Hq, Hkv, Sq, Skv, D, causal);
         if (bytes < 0) return PyLong_FromLongLong(bytes);
-        const at::Tensor dq = at::empty_like(q), dk = at::empty_like(k), dv = at::empty_like(v);
+        const at::Tensor dq = fresh(q.sizes(), at::kBFloat16, q), dk = fresh(k.sizes(), at::kBFloat16, q), dv = fresh(v.sizes(), at::kBFloat16, q);
         const int rc = launch(q, bytes, [&](void *stream, void *workspace) {
             return bwd(ptr(dout), (const float *)ptr(dlse), ptr(q), ptr(k), ptr(v), ptr(o), (const float *)ptr(lse), ptr(dq), ptr(dk), ptr(dv),
                        workspace, (size_t)bytes, B, Hq, Hkv, Sq, Skv, D, causal, scale, stream);
@@ -226,7 +235,7 @@ std::vector<at::Tensor> results(PyObject *out, const std::vector<at::Tensor> &li
 {
     std::vector<at::Tensor> all;
     if (out == Py_None) {
-        for (const at::Tensor &t : like) all.push_back(at::empty(t.sizes(), t.options()));
+        for (const at::Tensor &t : like) all.push_back(fresh(t.sizes(), t.scalar_type(), t));
         return all;
     }
     require(PyTuple_CheckExact(out) && PyTuple_GET_SIZE(out) == (Py_ssize_t)like.size());
@@ -288,7 +297,7 @@ PyObject *rope_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
         if (x.qw.defined()) {
             bytes = rope_workspace(&x.r);
             if (bytes < 0) return PyLong_FromLongLong(bytes);
-            for (at::Tensor &w : dw) w = at::empty({x.r.D}, x.q.options().dtype(at::kFloat));
+            for (at::Tensor &w : dw) w = fresh({x.r.D}, at::kFloat, x.q);
         }
         attn_heads h[8] = {};
         for (size_t i = 0; i < in.size(); ++i) {
