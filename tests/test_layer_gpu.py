@@ -379,6 +379,35 @@ def test_norm_rope_out_counts_as_written():
             call((out[0], out[0]))
 
 
+def test_threads_on_streams_of_their_own():
+    """Calls made at once, from several threads: workspaces and results of each are its own."""
+    import threading
+    do, q, k, v, o, lse, _ = cuda(*inputs(2, 4, 2, 260, 260, True, seed=5300))
+    w, (cos, sin) = torch.ones(128, device="cuda"), cuda(*L.table(260, 128))
+
+    def calls():
+        return (*A.attention_backward(do, q, k, v, o, lse, causal=True), *A.qk_norm_rope(q, k, w, w, cos, sin),
+                *A.qk_norm_rope_backward(do, k, q, k, w, w, cos, sin))
+
+    want, right = calls(), []
+    torch.cuda.synchronize()
+
+    def run(n):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(15):
+                got = calls()
+                torch.cuda.current_stream().synchronize()
+                if _equal(got, want):
+                    right.append(n)
+
+    threads = [threading.Thread(target=run, args=(n,)) for n in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(right) == 4 * 15
+
+
 # --------------------------------------------------------------------------------------------- native call and general form
 class Sub(torch.Tensor):
     pass
