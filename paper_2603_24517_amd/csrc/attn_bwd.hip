@@ -87,9 +87,8 @@ __device__ __forceinline__ int fast_div(int n, Div d) { return (int)((__umulhi((
 struct Role {
     int groups, tiles, splits;      // grid: groups x tiles x splits (the largest number of pieces)
     int most;
-    int window;                     // groups whose tiles are dealt out together
-    bool by_xcd;                    // an XCD keeps to its own groups
-    int items;
+    int items, per_xcd;             // of all XCDs and of one (of all, where they do not keep to their own groups)
+    int window, per_window;         // groups whose tiles are dealt out together, and their items
     Div d_window, d_per_tile, d_per_window;
 };
 struct Params {
@@ -103,6 +102,9 @@ struct Params {
     float c, scale;                 // c = scale * log2(e)
     float masked;                   // the score whose probability is 0: c * masked = -inf
     Role keys, rows;
+    int xcd_groups;                 // 0, or the K/V heads (of all batch entries) that each XCD keeps to
+    bool together;                  // behind each window's keys items come its rows items; otherwise all rows items come last
+    Div d_both;                     // items of a window, of both kinds
     Div d_hkv, d_chunks, d_g;
     int join_keys;                  // workgroups of attn_bwd_join for dk and dv
 };
@@ -573,33 +575,39 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     }
 }
 
-// Which item the n-th workgroup of a kind takes: longest tiles first.  The hardware deals workgroups round-robin to the 8 XCDs, each with an L2 of its own;
-// where the groups (batch entries x K/V heads) divide among them, an XCD keeps to its own groups, a window of them at a time, so that
-// the tiles of a group, which stream the same data, meet in one L2.
-__device__ __forceinline__ void find_item(const Role &r, int n, int &group, int &tile, int &piece)
+// Which item of a kind has number n in its order (together: in that of window w): window by window, longest tiles first.
+__device__ __forceinline__ void find_item(const Role &r, bool together, int n, int w, int first, int &group, int &tile, int &piece)
 {
-    int base = 0;
-    if (r.by_xcd) {
-        base = (n & 7) * (r.groups >> 3);
-        n >>= 3;
+    if (!together) {
+        w = fast_div(n, r.d_per_window);
+        n -= w * r.per_window;
     }
-    const int w = fast_div(n, r.d_per_window);
-    n -= w * r.window * r.tiles * r.splits;
     tile = fast_div(n, r.d_per_tile);
     n -= tile * r.window * r.splits;
     piece = fast_div(n, r.d_window);
-    group = base + w * r.window + n - piece * r.window;
+    group = first + w * r.window + n - piece * r.window;
 }
 
+// The hardware deals workgroups round-robin to the 8 XCDs, each with an L2 of its own; where the groups (batch entries x K/V heads) divide among them, an
+// XCD keeps to its own groups, a window of them at a time, so that the tiles of a group, which stream the same data, meet in one L2.
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_bwd_kernel(const Params p)
 {
-    const int n = blockIdx.x;
+    int n = blockIdx.x, first = 0, w = 0, of_keys = p.keys.per_xcd;
+    if (p.xcd_groups) {
+        first = (n & 7) * p.xcd_groups;
+        n >>= 3;
+        if (p.together) {
+            w = fast_div(n, p.d_both);
+            of_keys = p.keys.per_window;
+            n -= w * (of_keys + p.rows.per_window);
+        }
+    }
     int group, tile, piece;
-    if (n < p.keys.items) {
-        find_item(p.keys, n, group, tile, piece);
+    if (n < of_keys) {
+        find_item(p.keys, p.together, n, w, first, group, tile, piece);
         item<true>(p, group, tile, piece);
     } else {
-        find_item(p.rows, n - p.keys.items, group, tile, piece);
+        find_item(p.rows, p.together, n - of_keys, w, first * p.chunks, group, tile, piece);
         item<false>(p, group, p.rows.tiles - 1 - tile, piece);
     }
 }
@@ -664,25 +672,56 @@ constexpr int CUS = 256, PLACES = 2 * CUS;
 // up to 90 ways: the choice is 2.1 % off the best of those on average, 18 % at most.
 constexpr double KEYS_STEP = 0.75, ROWS_STEP = 0.69, SHARED = 1.38, ITEM = 3.8, LAST = 0.7, JOIN = 4.6, JOIN_BYTES = 7.9e6;
 constexpr int MOST_PIECES = 32;
+constexpr double CACHE_BYTES = 192e6;      // three quarters of the memory-side cache
 
-void deal(Role &r)
+// The order of the items.  Windows are as many groups as an XCD's 64 places take, or a few more, so that windows are equal.
+int fit_window(int groups, int per_group)
 {
-    r.items = r.groups * r.tiles * r.splits;
-    r.by_xcd = r.groups % 8 == 0;
-    r.window = r.groups;
-    if (r.by_xcd) {
-        // all groups of an XCD at once, longest tiles first, while that is few rounds; then as many as its 64 places take, or a few more, so that
-        // windows are equal
-        const int per_xcd = r.groups / 8, per_group = r.tiles * r.splits;
-        r.window = per_xcd;
-        if ((long long)per_xcd * per_group > 4 * PLACES / 8) {
-            r.window = (PLACES / 8 + per_group - 1) / per_group;
-            while (per_xcd % r.window) ++r.window;
+    int window = (PLACES / 8 + per_group - 1) / per_group;
+    if (window > groups) return groups;
+    while (groups % window) ++window;
+    return window;
+}
+void deal(Params &p)
+{
+    const int groups = p.keys.groups, both = p.keys.tiles * p.keys.splits + p.chunks * p.rows.tiles * p.rows.splits;
+    p.xcd_groups = groups % 8 == 0 ? groups / 8 : 0;
+    // Keys and rows items read the same inputs.  Side by side they find them in L2, which pays where a few tiles to a group leave the rest of the
+    // traffic to memory and the cache behind the L2s does not hold the inputs, unless an item is so long that it must not start late: more than a
+    // quarter of a place's work.  Together / apart, inputs from memory, us: 96 x 300, 16 heads, masked 347 / 387; 210 x 198, 8 heads, masked 228 / 252;
+    // 27 x 642, 24 heads 589 / 626; 34 x 840, 32 on 8 heads 1414 / 1555; longer items 4 x 2401, 32 on 4, masked 877 / 753; smaller inputs 512 x 64, 4 heads,
+    // masked 89 / 86.  Of 60 calls drawn 27 are dealt together: 4.4 % faster on average, between 11 % faster and 1.8 % slower.
+    p.together = false;
+    if (p.xcd_groups && both < PLACES / 8 && 2.0 * ROW_BYTES * ((double)p.G * p.Sq + p.Skv) * groups > CACHE_BYTES) {
+        double all = 0;
+        int longest = 0;
+        for (int t = 0; t < p.keys.tiles; ++t) {
+            const int n = keys_steps(p, t);
+            all += n;
+            longest = n > longest ? n : longest;
         }
+        for (int t = 0; t < p.rows.tiles; ++t) {
+            const int n = rows_steps(p, t);
+            all += (double)n * p.chunks;
+            longest = n > longest ? n : longest;
+        }
+        p.together = 4.0 * longest * PLACES <= all * groups;
     }
-    r.d_window = make_div(r.window);
-    r.d_per_tile = make_div(r.window * r.splits);
-    r.d_per_window = make_div(r.window * r.splits * r.tiles);
+    for (Role *r : {&p.keys, &p.rows}) {
+        const int heads = r == &p.keys ? 1 : p.chunks, per_group = r->tiles * r->splits;
+        r->items = r->groups * per_group;
+        r->per_xcd = p.xcd_groups ? r->items / 8 : r->items;
+        r->window = r->groups;
+        if (p.together)
+            r->window = fit_window(p.xcd_groups, both) * heads;
+        else if (p.xcd_groups)      // all groups of an XCD at once, longest tiles first, while that is few rounds
+            r->window = r->per_xcd <= 4 * PLACES / 8 ? p.xcd_groups * heads : fit_window(p.xcd_groups * heads, per_group);
+        r->per_window = r->window * per_group;
+        r->d_window = make_div(r->window);
+        r->d_per_tile = make_div(r->window * r->splits);
+        r->d_per_window = make_div(r->per_window);
+    }
+    p.d_both = make_div(p.keys.per_window + p.rows.per_window);
 }
 
 int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &r)
@@ -748,8 +787,7 @@ int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &r)
             p.rows.splits = pieces(long_r, p.rows.most);
         }
     }
-    deal(p.keys);
-    deal(p.rows);
+    deal(p);
     auto pad = [](size_t n) { return (n + 255) / 256 * 256; };
     r.stats = pad((size_t)B * Hq * p.qtiles * 2 * BT * sizeof(float));
     p.join_keys = p.keys.splits > 1 ? (int)nk * 8 : 0;
