@@ -507,6 +507,16 @@ def test_backward_of_many_short_sequences():
     assert ((dq.float() - want).abs() <= 2.1 * L.H * size + 2 * L.F * SCALE * (do.float().abs() * v.float().abs()).sum(-1, keepdim=True) * k.float().abs()).all()
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,Sq,Skv,causal", [(512, 8, 4, 62, 62, True), (96, 16, 16, 200, 200, True), (208, 12, 4, 90, 200, False)])
+def test_backward_of_large_batches_of_short_sequences(B, Hq, Hkv, Sq, Skv, causal):
+    """Inputs beyond every cache, whose two kinds of items are dealt side by side: three sequences, over and over."""
+    do, q, k, v, o, lse, _ = inputs(3, Hq, Hkv, Sq, Skv, causal, seed=5400)
+    at = torch.arange(B) % 3
+    got = A.attention_backward(*(t.cuda()[at.cuda()].contiguous() for t in (do, q, k, v, o, lse)), causal=causal)
+    L.check_backward([x[:3] for x in got], L.backward64(do, q, k, v, o, lse, causal, SCALE))
+    assert all(torch.equal(x, x[at.cuda()]) for x in got)
+
+
 def test_norm_rope_beyond_32_bit_offsets():
     S, Hq, Hkv = 70000, 256, 1
     q, k = _device_rand(20, 1, S, Hq, 128), _device_rand(21, 1, S, Hkv, 128)
