@@ -87,15 +87,19 @@ def build_layer(verbose=False):
     return _hipcc([], LAYER_LIB, LAYER_SRCS, verbose)
 
 
-def build_call(verbose=False, src=CALL_SRC, out=CALL_LIB):
-    """A native part of the Python binding: host code against torch's headers and libraries."""
+def call_command(src, out):
+    """The compiler's command for a native part of the Python binding: host code against torch's headers and libraries."""
     import sysconfig
     import torch
     root = os.path.dirname(torch.__file__)
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{root}/include", f"-I{root}/include/torch/csrc/api/include",
-           "-I/opt/rocm/include", f"-I{sysconfig.get_paths()['include']}", "-o", out, src, f"-L{root}/lib", f"-Wl,-rpath,{root}/lib",
-           "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip"]
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{root}/include", f"-I{root}/include/torch/csrc/api/include",
+            "-I/opt/rocm/include", f"-I{sysconfig.get_paths()['include']}", "-o", out, src, f"-L{root}/lib", f"-Wl,-rpath,{root}/lib",
+            "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip"]
+
+
+def build_call(verbose=False, src=CALL_SRC, out=CALL_LIB):
+    cmd = call_command(src, out)
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)

@@ -75,6 +75,12 @@ at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor &q
     return at::Tensor(at::detail::empty_cuda(sizes, type, q.device(), std::nullopt));
 }
 
+// The interpreter's lock given back, and taken again however the block ends.
+struct Unlocked {
+    PyThreadState *const state = PyEval_SaveThread();
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
 // f(stream, workspace), without the interpreter's lock, with q's device current.  The workspace, if any, comes from torch's allocator, as a tensor's
 // memory would: it belongs to the stream, and goes back to it when the call has been enqueued.
 template <class F>
@@ -86,9 +92,8 @@ int launch(const at::Tensor &q, long long bytes, F &&f)
         void *stream = (void *)c10::hip::getCurrentHIPStream(index).stream();
         c10::DataPtr workspace;
         if (bytes > 0) workspace = c10::hip::HIPCachingAllocator::get()->allocate((size_t)bytes);
-        Py_BEGIN_ALLOW_THREADS
+        const Unlocked unlocked;
         rc = f(stream, workspace.get());
-        Py_END_ALLOW_THREADS
     };
     if (index == c10::hip::current_device()) {
         go();
@@ -157,9 +162,12 @@ PyObject *backward(PyObject *, PyObject *const *args, Py_ssize_t n)
         const long long bytes = bwd_workspace(B, Hq, Hkv, Sq, Skv, D, causal);
         if (bytes < 0) return PyLong_FromLongLong(bytes);
         const at::Tensor dq = fresh(q.sizes(), at::kBFloat16, q), dk = fresh(k.sizes(), at::kBFloat16, q), dv = fresh(v.sizes(), at::kBFloat16, q);
+        // (addresses with the lock held: torch throws for a tensor without storage, a functorch wrapper say)
+        void *const in[] = {ptr(dout), ptr(q), ptr(k), ptr(v), ptr(o)}, *const out[] = {ptr(dq), ptr(dk), ptr(dv)};
+        const float *const figures[] = {(const float *)ptr(dlse), (const float *)ptr(lse)};
         const int rc = launch(q, bytes, [&](void *stream, void *workspace) {
-            return bwd(ptr(dout), (const float *)ptr(dlse), ptr(q), ptr(k), ptr(v), ptr(o), (const float *)ptr(lse), ptr(dq), ptr(dk), ptr(dv),
-                       workspace, (size_t)bytes, B, Hq, Hkv, Sq, Skv, D, causal, scale, stream);
+            return bwd(in[0], figures[0], in[1], in[2], in[3], in[4], figures[1], out[0], out[1], out[2], workspace, (size_t)bytes, B, Hq, Hkv, Sq, Skv, D,
+                       causal, scale, stream);
         });
         return rc != 0 ? PyLong_FromLong(rc) : tuple({dq, dk, dv});
     });
@@ -306,8 +314,9 @@ PyObject *rope_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
         }
         h[3] = heads(x.q);
         h[4] = heads(x.k);
+        float *const weights[] = {(float *)ptr(dw[0]), (float *)ptr(dw[1])};
         const int rc = launch(x.q, bytes, [&](void *stream, void *workspace) {
-            return rope_bwd(&x.r, h, h + 1, h + 2, h + 3, h + 4, h + 5, h + 6, h + 7, (float *)ptr(dw[0]), (float *)ptr(dw[1]), workspace, (size_t)bytes, stream);
+            return rope_bwd(&x.r, h, h + 1, h + 2, h + 3, h + 4, h + 5, h + 6, h + 7, weights[0], weights[1], workspace, (size_t)bytes, stream);
         });
         if (rc != 0) return PyLong_FromLong(rc);
         written(args[12], out);

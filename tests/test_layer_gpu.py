@@ -533,3 +533,15 @@ def test_norm_rope_beyond_32_bit_offsets():
     (ref, bound), (dw, dw_bound) = L.norm_rope_backward64(dq[:, at].cpu(), q[:, at].cpu(), w.cpu(), cos.cpu(), sin.cpu(), places, 1e-6, False)
     L.check_close(dx[:, at], (ref, bound))
     L.check_close(dqw, (dw, dw_bound))
+
+
+def test_calls_inside_torch_func_raise():
+    """torch.func hands on tensors without storage: torch's own exception for those, and the next call is none the worse."""
+    do, q, k, v, o, lse, _ = cuda(*inputs(1, 2, 1, 40, 40, True, seed=6200))
+    cos, sin = cuda(*L.table(40, 128))
+    want = A.attention_backward(do, q, k, v, o, lse, causal=True)
+    for call in (lambda x: A.attention_backward(do, x, k, v, o, lse, causal=True)[0], lambda x: A.qk_norm_rope(x, k, None, None, cos, sin)[0],
+                 lambda x: A.qk_norm_rope_backward(x, k, q, k, None, None, cos, sin)[0]):
+        with pytest.raises(RuntimeError, match="storage"):
+            torch.func.grad(lambda x: call(x).float().sum())(q)
+    assert _equal(A.attention_backward(do, q, k, v, o, lse, causal=True), want)
