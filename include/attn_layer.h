@@ -95,8 +95,9 @@ int attn_qk_norm_rope(const attn_rope *r, const attn_heads *q_in, const attn_hea
  * attn_qk_norm_rope_bwd -- the gradient of attn_qk_norm_rope: from dq_out, dk_out (and dv_out, where given) and the inputs
  * q_in, k_in to dq_in, dk_in (and dv_in, a copy).  With z the rotated gradient turned back, xhat = x / sqrt(mean(x^2) + eps):
  *     dweight = sum over tokens and heads of z * xhat      dx = (z w - xhat * mean(z w xhat)) / sqrt(mean(x^2) + eps)
- * dq_weight and dk_weight: FP32 [D], fully overwritten; both NULL if they are not wanted.  The sums are FP32 in a fixed
- * order.  workspace: attn_qk_norm_rope_bwd_workspace(r) bytes, 16-byte aligned, if dq_weight is given.
+ * A token whose place lies outside the table, whose q and k were NaN whatever the inputs and weights, gets NaN in dq_in and dk_in and
+ * is left out of the sums.  dq_weight and dk_weight: FP32 [D], fully overwritten; both NULL if they are not wanted.  The sums are FP32
+ * in a fixed order.  workspace: attn_qk_norm_rope_bwd_workspace(r) bytes, 16-byte aligned, if dq_weight is given.
  */
 int attn_qk_norm_rope_bwd(const attn_rope *r, const attn_heads *dq_out, const attn_heads *dk_out, const attn_heads *dv_out,
                           const attn_heads *q_in, const attn_heads *k_in, const attn_heads *dq_in, const attn_heads *dk_in,

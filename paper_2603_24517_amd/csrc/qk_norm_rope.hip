@@ -242,12 +242,13 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(const Params p)
         lane.load(place(k.z, at.b, at.s, at.h), z);
         const bool inside = angles(p, at, lane.j, lane.turns, c, s);
         const float r = inside ? reciprocal_rms(x, p.eps) : NAN;
+        const bool counts = at.real && inside;      // a token without a place is NaN whatever the weights are: no gradient of theirs
         lane.template turn<true>(z, c, s);
         float m = 0.0f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             x[e] *= r;                                      // xhat
-            if (at.real) dw[e] = fmaf(z[e], x[e], dw[e]);
+            if (counts) dw[e] = fmaf(z[e], x[e], dw[e]);
             z[e] *= w[e];
             m = fmaf(z[e], x[e], m);
         }

@@ -284,7 +284,7 @@ def qk_norm_rope_backward(dq, dk, q, k, q_weight, k_weight, cos, sin, positions=
     Arguments as there; dq, dk, dv: BF16, of the shapes of q and k, last dimension contiguous.  Returns (dq, dk, dq_weight, dk_weight)
     or, with dv, (dq, dk, dv, dq_weight, dk_weight): BF16 like the inputs, contiguous or in the tensors `out` (the slices of
     the gradient of one projection, say), which must not share memory with each other or with the inputs; the weights' gradients
-    FP32 [D], None without weights.
+    FP32 [D], None without weights.  A token whose place lies outside the table gets NaN in dq and dk and is left out of the weights' gradients.
     """
     if out is not None:
         out = tuple(out)

@@ -289,6 +289,29 @@ def test_norm_rope_places_outside_the_table():
     assert torch.isnan(x[:, 1::2].float()).all() and not torch.isnan(x[:, ::2].float()).any()
 
 
+@pytest.mark.parametrize("S,dtype", [(4, torch.int32), (4, torch.int64), (700, torch.int64)])
+def test_norm_rope_backward_of_places_outside_the_table(S, dtype):
+    """NaN in these tokens' own gradients; the weights' gradients are those of the other tokens, whatever arrives for these."""
+    q, k, dq, dk = (L.rand(30 + n, 2, S, h, 128) for n, h in enumerate((3, 1, 3, 1)))
+    g = torch.Generator().manual_seed(34)
+    qw, kw = ((1 + 0.3 * torch.randn(128, generator=g)) for _ in range(2))
+    cos, sin = L.table(S, 64)
+    pos = torch.arange(S).repeat(2, 1).to(dtype)
+    pos[0, 1], pos[1, 2] = -1, S
+    if dtype == torch.int64:
+        pos[0, 3] = 1 << 40
+    out = (pos < 0) | (pos >= S)
+    dq[0, 1] = 0.0
+    dk[1, 2] = math.nan
+    got = A.qk_norm_rope_backward(*cuda(dq, dk, q, k, qw, kw, cos, sin, pos))
+    at = torch.where(out, 0, pos).long()
+    for x, dw, dz, t, w, name in ((got[0], got[2], dq, q, qw, "q"), (got[1], got[3], dk, k, kw, "k")):
+        assert torch.isnan(x[out.cuda()].float()).all()
+        (ref, bound), (ref_w, bound_w) = L.norm_rope_backward64(dz.masked_fill(out[:, :, None, None], 0.0), t, w, cos, sin, at, 1e-6, False)
+        L.check_close(x[~out.cuda()], (ref[~out], bound[~out]), f"d{name}")
+        L.check_close(dw, (ref_w, bound_w), f"d{name}_weight")
+
+
 def test_norm_rope_zeros_and_extremes():
     """Rows of zeros (with eps; their gradient is that of x / sqrt(eps)), and rows whose squares leave BF16's but not FP32's precision."""
     q = torch.zeros(1, 3, 2, 128, dtype=torch.bfloat16)
