@@ -37,8 +37,11 @@
 
 #include "../../include/attn.h"
 #include "../../include/attn_layer.h"
+#include "attn_bwd_plan.h"
 
 namespace {
+
+using namespace attn_bwd_plan;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -50,13 +53,8 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #define LDS_AS __attribute__((address_space(3)))
 
-constexpr int HD = 128;
-constexpr int ROW_BYTES = HD * 2;
-constexpr int BT = 32;                          // streamed rows per step
 constexpr int TILE_BYTES = BT * ROW_BYTES;      // 8 KiB
-constexpr int ITEM_ROWS = 128;                  // held rows of an item, 32 per wavefront
 constexpr int STATS_BYTES = 2 * BT * 4;         // -LSE and -delta of a step's 32 rows
-constexpr size_t PART_BYTES = 32 * HD * sizeof(float);     // what one wavefront leaves of one sum
 constexpr float LOG2E = 1.4426950408889634f;
 
 // How an item of each kind uses LDS: a ring of stages, each a tile of Y1 and one of Y2 (keys items: and its rows' figures).  While step j runs, step
@@ -72,63 +70,21 @@ struct Lds {
 constexpr int LDS_BYTES = Lds<true>::BYTES > Lds<false>::BYTES ? Lds<true>::BYTES : Lds<false>::BYTES;
 static_assert(LDS_BYTES <= 80 * 1024);
 
-// n / d for n < 2^31 with constants found on the host
-struct Div { uint32_t mul, shift; };
-__host__ inline Div make_div(uint32_t d)
-{
-    uint32_t l = 0;
-    while ((1ull << l) < d) ++l;
-    return {(uint32_t)(((1ull << 32) * ((1ull << l) - d)) / d + 1), l};
-}
-__device__ __forceinline__ int fast_div(int n, Div d) { return (int)((__umulhi((uint32_t)n, d.mul) + (uint32_t)n) >> d.shift); }
-
-// The items of one kind.  A tile's steps (streamed tiles, of all heads of a group) are cut into pieces of at most `most`, so that a call of few or
-// uneven tiles fills the chip; a tile of several pieces leaves FP32 parts, which attn_bwd_join adds up.
-struct Role {
-    int groups, tiles, splits;      // grid: groups x tiles x splits (the largest number of pieces)
-    int most;
-    int items, per_xcd;             // of all XCDs and of one (of all, where they do not keep to their own groups)
-    int window, per_window;         // groups whose tiles are dealt out together, and their items
-    Div d_window, d_per_tile, d_per_window;
-};
-struct Params {
+struct Tensors {
     const __bf16 *q, *k, *v, *dout;
     __bf16 *dq, *dk, *dv;
     const float *stats;
     unsigned char *part_q, *part_kv;    // parts: [tile][group][piece][wavefront] PART_BYTES each; of keys items twice that, dk and dv
-    int B, Hq, Hkv, Sq, Skv, G, qtiles;
-    int pack_log2, chunks;          // rows items: query heads of a group side by side, and how many such chunks a group has
-    int off;                        // key j valid for row i iff j <= i + off (without the mask: always true)
     float c, scale;                 // c = scale * log2(e)
     float masked;                   // the score whose probability is 0: c * masked = -inf
-    Role keys, rows;
-    int xcd_groups;                 // 0, or the K/V heads (of all batch entries) that each XCD keeps to
-    bool together;                  // behind each window's keys items come its rows items; otherwise all rows items come last
-    Div d_both;                     // items of a window, of both kinds
-    Div d_hkv, d_chunks, d_g;
-    int join_keys;                  // workgroups of attn_bwd_join for dk and dv
 };
+struct Params : Tensors, Sizes {};
 
 // f(0), f(1), ... f(N - 1) with constants (the unroller gives up on a loop of this size)
 template <int... I, class F>
 __device__ __forceinline__ void static_for(std::integer_sequence<int, I...>, F &&f) { (f(std::integral_constant<int, I>{}), ...); }
 template <int N, class F>
 __device__ __forceinline__ void static_for(F &&f) { static_for(std::make_integer_sequence<int, N>{}, f); }
-
-// Query tiles in front of a tile's first key (keys items); steps of a tile.
-__host__ __device__ inline int keys_skip(const Params &p, int tile)
-{
-    const int first = tile * ITEM_ROWS - p.off;             // first row that sees the tile's first key
-    return first > 0 ? (first / BT < p.qtiles ? first / BT : p.qtiles) : 0;
-}
-__host__ __device__ inline int keys_steps(const Params &p, int tile) { return (p.qtiles - keys_skip(p, tile)) * p.G; }
-__host__ __device__ inline int rows_steps(const Params &p, int tile)
-{
-    const int end = (tile + 1) * (ITEM_ROWS >> p.pack_log2);
-    const int last = (end < p.Sq ? end : p.Sq) - 1 + p.off;      // last key that the tile's last row sees
-    return last < 0 ? 0 : (last < p.Skv - 1 ? last : p.Skv - 1) / BT + 1;
-}
-__host__ __device__ inline int pieces(int steps, int most) { return steps <= most ? 1 : (steps + most - 1) / most; }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     bf16x2 p = __builtin_convertvector((f32x2){a, b}, bf16x2);   // v_cvt_pk_bf16_f32, nearest even
@@ -215,19 +171,6 @@ __global__ __launch_bounds__(256) void attn_bwd_stats(const __bf16 *dout, const 
 }
 
 // ------------------------------------------------------------------------------------------------------ the products
-// Batch entry, head and first of the 32 rows that a wavefront of an item holds.
-__device__ __forceinline__ void find_rows(const Params &p, bool keys, int group, int tile, int wave, int &b, int &head, int &x0)
-{
-    const int bh = keys ? group : fast_div(group, p.d_chunks);
-    b = fast_div(bh, p.d_hkv);
-    head = bh - b * p.Hkv;
-    x0 = tile * ITEM_ROWS + wave * 32;
-    if (!keys) {
-        head = head * p.G + ((group - bh * p.chunks) << p.pack_log2) + (wave & ((1 << p.pack_log2) - 1));
-        x0 = tile * (ITEM_ROWS >> p.pack_log2) + (wave >> p.pack_log2) * 32;
-    }
-}
-
 // One item: KEYS holds K (X1), V (X2) and streams Q (Y1), dO (Y2); otherwise the reverse.
 template <bool KEYS>
 __device__ __forceinline__ void item(const Params &p, int group, int tile, int piece)
@@ -249,10 +192,7 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     int steps = KEYS ? per_head * p.G : per_head, step0 = 0;
     const int n_pieces = pieces(steps, KEYS ? p.keys.most : p.rows.most);
     if (piece >= n_pieces) return;
-    if (n_pieces > 1) {
-        step0 = (int)((unsigned)steps * (unsigned)piece / (unsigned)n_pieces);
-        steps = (int)((unsigned)steps * (unsigned)(piece + 1) / (unsigned)n_pieces) - step0;
-    }
+    if (n_pieces > 1) piece_steps(steps, n_pieces, piece, step0, steps);
     // (all of it is wave-uniform: scalar registers)
     auto uniform = [](int &x) __attribute__((always_inline)) { x = __builtin_amdgcn_readfirstlane(x); };
     uniform(b); uniform(x_head); uniform(x0); uniform(steps);
@@ -575,41 +515,11 @@ __device__ __forceinline__ void item(const Params &p, int group, int tile, int p
     }
 }
 
-// Which item of a kind has number n in its order (together: in that of window w): window by window, longest tiles first.
-__device__ __forceinline__ void find_item(const Role &r, bool together, int n, int w, int first, int &group, int &tile, int &piece)
-{
-    if (!together) {
-        w = fast_div(n, r.d_per_window);
-        n -= w * r.per_window;
-    }
-    tile = fast_div(n, r.d_per_tile);
-    n -= tile * r.window * r.splits;
-    piece = fast_div(n, r.d_window);
-    group = first + w * r.window + n - piece * r.window;
-}
-
-// The hardware deals workgroups round-robin to the 8 XCDs, each with an L2 of its own; where the groups (batch entries x K/V heads) divide among them, an
-// XCD keeps to its own groups, a window of them at a time, so that the tiles of a group, which stream the same data, meet in one L2.
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_bwd_kernel(const Params p)
 {
-    int n = blockIdx.x, first = 0, w = 0, of_keys = p.keys.per_xcd;
-    if (p.xcd_groups) {
-        first = (n & 7) * p.xcd_groups;
-        n >>= 3;
-        if (p.together) {
-            w = fast_div(n, p.d_both);
-            of_keys = p.keys.per_window;
-            n -= w * (of_keys + p.rows.per_window);
-        }
-    }
-    int group, tile, piece;
-    if (n < of_keys) {
-        find_item(p.keys, p.together, n, w, first, group, tile, piece);
-        item<true>(p, group, tile, piece);
-    } else {
-        find_item(p.rows, p.together, n - of_keys, w, first * p.chunks, group, tile, piece);
-        item<false>(p, group, p.rows.tiles - 1 - tile, piece);
-    }
+    const Item x = which_item(p, blockIdx.x);
+    if (x.keys) item<true>(p, x.group, x.tile, x.piece);
+    else item<false>(p, x.group, x.tile, x.piece);
 }
 
 // The sum of the parts of each tile that was cut, in the order of its pieces.  A workgroup adds up one wavefront's 32 rows of one result: 8 elements
@@ -650,153 +560,6 @@ __global__ __launch_bounds__(256) void attn_bwd_join(const Params p)
 }
 
 // ----------------------------------------------------------------------------------------------------------- host
-struct Plan {
-    Params p;                                   // sizes and roles
-    size_t stats, part_kv, part_q, total;       // bytes: the workspace's three parts
-};
-
-int check_sizes(int B, int Hq, int Hkv, int Sq, int Skv, int D)
-{
-    if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Skv <= 0 || D <= 0) return ATTN_E_SHAPE;
-    if (Hq % Hkv != 0) return ATTN_E_SHAPE;
-    if (D != HD) return ATTN_E_UNSUPPORTED;
-    if ((long long)Sq + Skv >= (1ll << 31) - 1024 || Hq > 32768 || Hkv > 32768) return ATTN_E_UNSUPPORTED;
-    return ATTN_OK;
-}
-
-// Workgroups that are resident at a time on the device that this is written for, two per compute unit: how items are cut (and so what the
-// workspace needs) does not ask the device.
-constexpr int CUS = 256, PLACES = 2 * CUS;
-// Microseconds: a step alone on a compute unit, and how much longer it takes beside another; an item beside its steps; how much of the last items
-// stands out behind a full chip; the launch and the bytes per microsecond of adding up parts.  Fitted to 100 calls of this range, each cut in
-// up to 90 ways: the choice is 2.1 % off the best of those on average, 18 % at most.
-constexpr double KEYS_STEP = 0.75, ROWS_STEP = 0.69, SHARED = 1.38, ITEM = 3.8, LAST = 0.7, JOIN = 4.6, JOIN_BYTES = 7.9e6;
-constexpr int MOST_PIECES = 32;
-constexpr double CACHE_BYTES = 192e6;      // three quarters of the memory-side cache
-
-// The order of the items.  Windows are as many groups as an XCD's 64 places take, or a few more, so that windows are equal.
-int fit_window(int groups, int per_group)
-{
-    int window = (PLACES / 8 + per_group - 1) / per_group;
-    if (window > groups) return groups;
-    while (groups % window) ++window;
-    return window;
-}
-void deal(Params &p)
-{
-    const int groups = p.keys.groups, both = p.keys.tiles * p.keys.splits + p.chunks * p.rows.tiles * p.rows.splits;
-    p.xcd_groups = groups % 8 == 0 ? groups / 8 : 0;
-    // Keys and rows items read the same inputs.  Side by side they find them in L2, which pays where a few tiles to a group leave the rest of the
-    // traffic to memory and the cache behind the L2s does not hold the inputs, unless an item is so long that it must not start late: more than a
-    // quarter of a place's work.  Together / apart, inputs from memory, us: 96 x 300, 16 heads, masked 347 / 387; 210 x 198, 8 heads, masked 228 / 252;
-    // 27 x 642, 24 heads 589 / 626; 34 x 840, 32 on 8 heads 1414 / 1555; longer items 4 x 2401, 32 on 4, masked 877 / 753; smaller inputs 512 x 64, 4 heads,
-    // masked 89 / 86.  Of 60 calls drawn 27 are dealt together: 4.4 % faster on average, between 11 % faster and 1.8 % slower.
-    p.together = false;
-    if (p.xcd_groups && both < PLACES / 8 && 2.0 * ROW_BYTES * ((double)p.G * p.Sq + p.Skv) * groups > CACHE_BYTES) {
-        double all = 0;
-        int longest = 0;
-        for (int t = 0; t < p.keys.tiles; ++t) {
-            const int n = keys_steps(p, t);
-            all += n;
-            longest = n > longest ? n : longest;
-        }
-        for (int t = 0; t < p.rows.tiles; ++t) {
-            const int n = rows_steps(p, t);
-            all += (double)n * p.chunks;
-            longest = n > longest ? n : longest;
-        }
-        p.together = 4.0 * longest * PLACES <= all * groups;
-    }
-    for (Role *r : {&p.keys, &p.rows}) {
-        const int heads = r == &p.keys ? 1 : p.chunks, per_group = r->tiles * r->splits;
-        r->items = r->groups * per_group;
-        r->per_xcd = p.xcd_groups ? r->items / 8 : r->items;
-        r->window = r->groups;
-        if (p.together)
-            r->window = fit_window(p.xcd_groups, both) * heads;
-        else if (p.xcd_groups)      // all groups of an XCD at once, longest tiles first, while that is few rounds
-            r->window = r->per_xcd <= 4 * PLACES / 8 ? p.xcd_groups * heads : fit_window(p.xcd_groups * heads, per_group);
-        r->per_window = r->window * per_group;
-        r->d_window = make_div(r->window);
-        r->d_per_tile = make_div(r->window * r->splits);
-        r->d_per_window = make_div(r->per_window);
-    }
-    p.d_both = make_div(p.keys.per_window + p.rows.per_window);
-}
-
-int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &r)
-{
-    Params &p = r.p;
-    const int G = Hq / Hkv;
-    p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.Sq = Sq; p.Skv = Skv; p.G = G;
-    p.pack_log2 = G % 4 == 0 ? 2 : G % 2 == 0 ? 1 : 0;
-    p.chunks = G >> p.pack_log2;
-    p.qtiles = (Sq + BT - 1) / BT;
-    // (i + INT32_MAX - Sq - 256 is above every key for i >= 0 and within 32 bits for the i < Sq + 256 of a tile)
-    p.off = causal ? Skv - Sq : INT32_MAX - Sq - 256;
-    const int pos = ITEM_ROWS >> p.pack_log2;
-    const int tk = (Skv + ITEM_ROWS - 1) / ITEM_ROWS, tr = (Sq + pos - 1) / pos;
-    const long long nk = (long long)B * Hkv * tk, nr = (long long)B * Hkv * p.chunks * tr;
-    // (a launch has fewer than 2^32 threads; each 64 rows of the figures, with 32 of a head in line, take a workgroup of 256)
-    if (nk >= (1ll << 23) || nr >= (1ll << 23) || (long long)p.qtiles * BT * Hq >= (1ll << 30) / B || (long long)p.qtiles * G >= (1ll << 31))
-        return ATTN_E_UNSUPPORTED;
-    p.d_hkv = make_div(Hkv);
-    p.d_chunks = make_div(p.chunks);
-    p.d_g = make_div(G);
-    p.keys = {B * Hkv, tk, 1, INT32_MAX};
-    p.rows = {B * Hkv * p.chunks, tr, 1, INT32_MAX};
-
-    // Calls of few tiles for the chip, or of uneven ones, are cut: the pair of piece lengths whose estimate is the shortest.
-    const int long_k = keys_steps(p, 0), long_r = rows_steps(p, tr - 1), short_r = rows_steps(p, 0);
-    if (nk + nr < 4 * PLACES && (long long)long_k * MOST_PIECES < (1ll << 31)) {
-        double all_k = 0, all_r = 0;
-        for (int t = 0; t < tk; ++t) all_k += keys_steps(p, t);
-        for (int t = 0; t < tr; ++t) all_r += rows_steps(p, t);
-        all_k *= p.keys.groups;
-        all_r *= p.rows.groups;
-        const double kv_bytes = 2.0 * B * Skv * Hkv * HD * 4, q_bytes = (double)B * Sq * Hq * HD * 4;
-        double best = INFINITY;
-        int best_k = 1, best_r = 1;
-        for (int sk = 1; sk <= MOST_PIECES; sk += sk < 8 ? 1 : sk / 4) {
-            const int mk = (long_k + sk - 1) / sk;
-            if (sk > 1 && mk < 3) break;
-            for (int sr = 1; sr <= MOST_PIECES; sr += sr < 8 ? 1 : sr / 4) {
-                const int mr = (long_r + sr - 1) / sr;
-                if (sr > 1 && mr < 4) break;
-                const double pk = sk > 1 ? all_k / mk : nk, pr = sr > 1 ? all_r / mr : nr, n = pk + pr;       // pieces, about
-                const double more = n <= CUS ? 0 : n >= PLACES ? 1 : (n - CUS) / (PLACES - CUS), slow = 1 + (SHARED - 1) * more;
-                const double k = slow * KEYS_STEP, q = slow * ROWS_STEP, ik = ITEM + k * mk, ir = ITEM + q * mr;
-                double us = (all_k * k + all_r * q + n * ITEM) / PLACES;
-                if (n > PLACES) us += LAST * (ITEM + q * (sr > 1 ? mr : short_r));
-                if (us < ik) us = ik;
-                if (us < ir) us = ir;
-                if (sk > 1 || sr > 1) us += JOIN + 2 * ((sk > 1 ? sk * kv_bytes : 0) + (sr > 1 ? sr * q_bytes : 0)) / JOIN_BYTES;
-                if (us < best) {
-                    best = us;
-                    best_k = sk;
-                    best_r = sr;
-                }
-            }
-        }
-        if (best_k > 1) {
-            p.keys.most = (long_k + best_k - 1) / best_k;
-            p.keys.splits = pieces(long_k, p.keys.most);
-        }
-        if (best_r > 1) {
-            p.rows.most = (long_r + best_r - 1) / best_r;
-            p.rows.splits = pieces(long_r, p.rows.most);
-        }
-    }
-    deal(p);
-    auto pad = [](size_t n) { return (n + 255) / 256 * 256; };
-    r.stats = pad((size_t)B * Hq * p.qtiles * 2 * BT * sizeof(float));
-    p.join_keys = p.keys.splits > 1 ? (int)nk * 8 : 0;
-    r.part_kv = p.keys.splits > 1 ? (size_t)p.keys.items * 8 * PART_BYTES : 0;
-    r.part_q = p.rows.splits > 1 ? (size_t)p.rows.items * 4 * PART_BYTES : 0;
-    r.total = r.stats + r.part_kv + r.part_q;
-    return ATTN_OK;
-}
-
 bool launch(const void *kernel, dim3 grid, int threads, int lds, void **args, hipStream_t st)
 {
     if (hipLaunchKernel(kernel, grid, dim3(threads), args, lds, st) == hipSuccess) return true;
@@ -844,7 +607,7 @@ int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, 
     }
     hipStream_t st = (hipStream_t)stream;
 
-    Params &p = r.p;
+    Params p = {{}, r.p};
     p.q = (const __bf16 *)q; p.k = (const __bf16 *)k; p.v = (const __bf16 *)v; p.dout = (const __bf16 *)dout;
     p.dq = (__bf16 *)dq; p.dk = (__bf16 *)dk; p.dv = (__bf16 *)dv;
     p.stats = (const float *)workspace;
