@@ -41,8 +41,8 @@ extern "C" {
  *
  * Masked pairs take no part, whatever they hold, but for one thing: a value that is not finite in a row of q or dout, or of k,
  * makes the gradients of the keys, or queries, that are masked for it but lie within 160 positions of one that is not, NaN.
- * Size limits (ATTN_E_UNSUPPORTED): those of attn_fwd; B * Hkv * ceil(Skv / 128) and B * Hq * ceil(Sq / 128) below 2^23 and
- * B * Hq * Sq, with Sq rounded up to a multiple of 32, below 2^30.  ATTN_E_WORKSPACE if the workspace is too small.
+ * Size limits (ATTN_E_UNSUPPORTED): D, Sq + Skv, Hq and Hkv as in attn_fwd; B * Hkv * ceil(Skv / 128) and B * Hq / p * ceil(Sq * p / 128), p = 4, 2
+ * or 1 the largest that divides Hq / Hkv, below 2^23.  ATTN_E_WORKSPACE if the workspace is too small.
  */
 int attn_bwd(const void *dout, const float *dlse, const void *q, const void *k, const void *v, const void *o,
              const float *lse, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes,

@@ -218,10 +218,12 @@ inline int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &
     p.off = causal ? Skv - Sq : INT32_MAX - Sq - 256;
     const int pos = ITEM_ROWS >> p.pack_log2;
     const int tk = (Skv + ITEM_ROWS - 1) / ITEM_ROWS, tr = (Sq + pos - 1) / pos;
+    // A rows item holds rows of 4 heads at most: 2^25 heads or more are 2^23 items or more, and below that no product here leaves 64 bits.
+    if ((long long)B * Hq >= (1ll << 25)) return ATTN_E_UNSUPPORTED;
     const long long nk = (long long)B * Hkv * tk, nr = (long long)B * Hkv * p.chunks * tr;
-    // (a launch has fewer than 2^32 threads; each 64 rows of the figures, with 32 of a head in line, take a workgroup of 256)
-    if (nk >= (1ll << 23) || nr >= (1ll << 23) || (long long)p.qtiles * BT * Hq >= (1ll << 30) / B || (long long)p.qtiles * G >= (1ll << 31))
-        return ATTN_E_UNSUPPORTED;
+    // (A launch has fewer than 2^32 threads.  Fewer than 2^23 rows items also bound the rows with figures, 32 of a head in line, to less than 2^30, four
+    // threads each, and the steps of a keys tile to less than 2^25)
+    if (nk >= (1ll << 23) || nr >= (1ll << 23)) return ATTN_E_UNSUPPORTED;
     p.d_hkv = make_div(Hkv);
     p.d_chunks = make_div(p.chunks);
     p.d_g = make_div(G);
@@ -230,7 +232,7 @@ inline int make_plan(int B, int Hq, int Hkv, int Sq, int Skv, int causal, Plan &
 
     // Calls of few tiles for the chip, or of uneven ones, are cut: the pair of piece lengths whose estimate is the shortest.
     const int long_k = keys_steps(p, 0), long_r = rows_steps(p, tr - 1), short_r = rows_steps(p, 0);
-    if (nk + nr < 4 * PLACES && (long long)long_k * MOST_PIECES < (1ll << 31)) {
+    if (nk + nr < 4 * PLACES) {
         double all_k = 0, all_r = 0;
         for (int t = 0; t < tk; ++t) all_k += keys_steps(p, t);
         for (int t = 0; t < tr; ++t) all_r += rows_steps(p, t);

@@ -69,3 +69,36 @@ def test_every_item_of_drawn_calls_is_dealt_once(lib, plan, seed):
         B = int(2 ** rng.uniform(0, min(10.0, max(0.0, 22 - (Sq + Skv).bit_length() - Hq.bit_length()))))
         call = (B, Hq, Hkv, Sq, Skv, rng.random() < 0.6)
         assert lib.deal_check(_call(*call)) == 0, call
+
+
+@pytest.fixture(scope="module")
+def checked(tmp_path_factory):
+    """The plan in a program that ends where signed arithmetic overflows."""
+    exe = str(tmp_path_factory.mktemp("bwd_plan") / "plan")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-DPLAN_MAIN", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-o", exe, SHIM], check=True)
+
+    def run(calls):
+        text = "".join(" ".join(str(int(x)) for x in c) + "\n" for c in calls)
+        out = subprocess.run([exe], input=text, capture_output=True, text=True, timeout=60)
+        assert out.returncode == 0, out.stderr
+        return [int(x) for x in out.stdout.split()]
+    return run
+
+
+def _within_limits(B, Hq, Hkv, Sq, Skv, causal):
+    G = Hq // Hkv
+    p = 4 if G % 4 == 0 else 2 if G % 2 == 0 else 1
+    return (Sq + Skv < 2 ** 31 - 1024 and Hq <= 32768 and B * Hkv * -(-Skv // 128) < 2 ** 23 and B * Hq // p * -(-Sq // (128 // p)) < 2 ** 23)
+
+
+EDGES = [1, 2, 31, 32, 33, 127, 128, 129, 2 ** 15, 2 ** 16 - 1, 2 ** 23 - 1, 2 ** 23, 2 ** 25, 2 ** 29, 2 ** 30, 2 ** 31 - 1026, 2 ** 31 - 1]
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_sizes_at_the_limits(checked, causal):
+    """All products of the largest arguments: refused or planned as the header says, without a signed overflow on the way."""
+    heads = [(1, 1), (2, 1), (4, 1), (32768, 1), (32768, 32768), (3, 3), (32, 8)]
+    calls = [(B, *h, Sq, Skv, causal) for B in EDGES for h in heads for Sq in EDGES for Skv in EDGES]
+    got = checked(calls)
+    for c, rc in zip(calls, got):
+        assert rc == (A.ATTN_OK if _within_limits(*c) else A.ATTN_E_UNSUPPORTED), (c, rc)
