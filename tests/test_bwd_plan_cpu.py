@@ -102,3 +102,22 @@ def test_sizes_at_the_limits(checked, causal):
     got = checked(calls)
     for c, rc in zip(calls, got):
         assert rc == (A.ATTN_OK if _within_limits(*c) else A.ATTN_E_UNSUPPORTED), (c, rc)
+
+
+@pytest.mark.parametrize("xcd_groups", [5, 7, 11, 13, 62, 97, 101, 2 * 53, 3 * 37, 131, 997, 131071])
+@pytest.mark.parametrize("S", [64, 300, 1000, 4096])
+def test_windows_of_group_counts_without_divisors(plan, lib, xcd_groups, S):
+    """An XCD's 64 places are not asked to take more than twice their items at a time because its groups divide badly, nor to look for divisors."""
+    if S > 64 and xcd_groups > 1000:
+        pytest.skip("more items than a call may have")
+    call = (xcd_groups, 8, 8, S, S, False)
+    p = plan(*call)
+    assert p["xcd_groups"] == xcd_groups
+    tiles = -(-S // 128)
+    per_group = 2 * tiles if p["together"] else tiles
+    if p["together"] or xcd_groups * tiles > 4 * 64:
+        wanted = -(-64 // per_group)
+        assert wanted <= p["keys_window"] <= max(wanted, 2 * wanted - 1) or xcd_groups < 2 * wanted, p
+        assert p["rows_window"] == p["keys_window"]
+    assert lib.deal_check(_call(*call)) == 0
+    assert lib.plan_seconds(_call(*call)) < 100e-6       # (the search for a divisor took 500 us and more of the longest here)

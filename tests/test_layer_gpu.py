@@ -568,3 +568,17 @@ def test_calls_inside_torch_func_raise():
         with pytest.raises(RuntimeError, match="storage"):
             torch.func.grad(lambda x: call(x).float().sum())(q)
     assert _equal(A.attention_backward(do, q, k, v, o, lse, causal=True), want)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,Sq,Skv,causal", [(13, 8, 8, 600, 600, True), (11, 16, 8, 1300, 1300, True), (97, 8, 8, 300, 300, True), (29, 8, 8, 450, 700, False)])
+def test_backward_of_group_counts_without_divisors(B, Hq, Hkv, Sq, Skv, causal):
+    """Windows of groups, the last one longer than the others, each kind of items by itself and both side by side: two sequences, over and over."""
+    do, q, k, v, o, lse, _ = inputs(2, Hq, Hkv, Sq, Skv, causal, seed=5500)
+    at = (torch.arange(B) % 2).cuda()
+    got = A.attention_backward(*(t.cuda()[at].contiguous() for t in (do, q, k, v, o, lse)), causal=causal)
+    G = Hq // Hkv
+    for h in (0, Hkv - 1):          # (the 64-bit form of two heads)
+        part = slice(h * G, h * G + G)
+        few = (do[:, :, part], q[:, :, part], k[:, :, h:h + 1], v[:, :, h:h + 1], o[:, :, part], lse[:, part])
+        L.check_backward((got[0][:2, :, part], got[1][:2, :, h:h + 1], got[2][:2, :, h:h + 1]), L.backward64(*few, causal, SCALE))
+    assert all(torch.equal(x, x[at]) for x in got)
