@@ -142,3 +142,52 @@ def check_close(got, want, what=""):
     err = (got.cpu().double() - ref).abs()
     assert not torch.isnan(err).any(), f"{what}: NaN"
     assert (err <= bound).all(), f"{what}: {(err / bound).max().item():.2f} times the bound"
+
+
+# ------------------------------------------------------------------------------------------------- against differences of the forward
+def forward_exact(q, k, v, causal, scale):
+    """(O, LSE, P) in 64 bits, nothing rounded; CPU tensors, O [B, S, H, D], P [B, H, Sq, Skv]."""
+    G = q.shape[2] // k.shape[2]
+    q, k, v = (t.double().transpose(1, 2) for t in (q, k.repeat_interleave(G, 2), v.repeat_interleave(G, 2)))
+    s = torch.matmul(q, k.transpose(2, 3).contiguous()) * scale
+    s = s.masked_fill(~valid_pairs(q.shape[2], k.shape[2], causal), -math.inf)
+    lse = torch.logsumexp(s, -1)
+    p = torch.exp(s - torch.where(torch.isneginf(lse), 0.0, lse)[..., None])
+    return torch.matmul(p, v).transpose(1, 2), lse, p
+
+
+def check_slopes(grads, do, dlse, q, k, v, causal, scale):
+    """Gradients of sum(do O) + sum(dlse LSE), from the forward kernel's O and LSE, against differences of that number in 64 bits: along the signs of
+    the gradient itself, and of the shares in it that come through O and through LSE, so that all elements of one add up and a factor, a sign or a
+    lost term cannot hide.  The tolerance comes from the 64-bit gradient alone: `bound` of backward64 for each element; and delta's share of the
+    forward kernel's roundings, of its probabilities and of O, each at most H, which reaches all pairs of a row.  (Differences of steps h of a smooth
+    function are off by h^2: 1e-6 of the slope has room for it.)"""
+    o, lse, p = forward_exact(q, k, v, causal, scale)
+    ref, bound, _ = backward64(do, q, k, v, o, lse, causal, scale, dlse)
+    without_o, without_lse = (backward64(do, q, k, v, x, lse, causal, scale, y)[0] for x, y in ((torch.zeros_like(o), dlse), (o, None)))
+    G = q.shape[2] // k.shape[2]
+    kk, vv = k.double().repeat_interleave(G, 2), v.double().repeat_interleave(G, 2)
+    size = torch.matmul(p, vv.abs().transpose(1, 2)).transpose(1, 2) + o.abs()
+    delta = H * (do.double().abs() * size).sum(-1).transpose(1, 2)         # [B, H, Sq]
+
+    def value(q, k, v):
+        o, l, _ = forward_exact(q, k, v, causal, scale)
+        return (do.double() * o).sum().item() + (dlse.double() * l)[torch.isfinite(l)].sum().item()
+
+    for n, name in enumerate(("dq", "dk", "dv")):
+        shares = {"": ref[n]} if n == 2 else {"": ref[n], " through O": ref[n] - without_o[n], " through LSE": ref[n] - without_lse[n]}
+        for share, part in shares.items():
+            way = torch.sign(part)
+            at, h = [q.double(), k.double(), v.double()], 1e-5
+            up, down = (at[:n] + [at[n] + s * h * way] + at[n + 1:] for s in (1, -1))
+            slope = (value(*up) - value(*down)) / (2 * h)
+            # what an error of delta does along `way`
+            s = torch.zeros_like(p)
+            if n == 0:
+                s = torch.matmul(way.transpose(1, 2), kk.transpose(1, 2).transpose(2, 3).contiguous())
+            elif n == 1:
+                s = torch.matmul(q.double().transpose(1, 2), way.repeat_interleave(G, 2).transpose(1, 2).transpose(2, 3).contiguous())
+            tolerance = bound[n].sum().item() + (delta * (abs(scale) * p * s).sum(-1).abs()).sum().item() + 1e-6 * ref[n].abs().sum().item()
+            got = (grads[n].cpu().double() * way).sum().item()
+            assert tolerance <= 0.6 * part.abs().sum().item(), f"{name}{share}: too much room, {tolerance} of {part.abs().sum().item()}"
+            assert abs(got - slope) <= tolerance, f"{name}{share}: {got} along its signs, differences {slope}, tolerance {tolerance}"

@@ -164,6 +164,27 @@ def test_backward_reference_against_autograd(Sq, Skv, causal, Hq, Hkv):
         torch.testing.assert_close(a, b, rtol=1e-10, atol=1e-10)
 
 
+def test_differences_reject_wrong_gradients():
+    """check_slopes, which the GPU tests hold the kernel's gradients against, takes rounded gradients and refuses scaled, negated and incomplete ones."""
+    Hq, Hkv, S, scale = 4, 2, 150, 128 ** -0.5
+    do, dl = L.rand(1, 1, S, Hq, 128), L.rand(2, 1, Hq, S, mul=4.0).float()
+    q, k, v = L.rand(3, 1, S, Hq, 128), L.rand(4, 1, S, Hkv, 128), L.rand(5, 1, S, Hkv, 128)
+    o, lse = L.forward64(q, k, v, True, scale)
+    good = [t.to(torch.bfloat16) for t in L.backward64(do, q, k, v, o, lse, True, scale, dl)[0]]
+    L.check_slopes(good, do, dl, q, k, v, True, scale)
+    for n, name in enumerate(("dq", "dk", "dv")):
+        for factor in (0.0, 0.5, 0.75, 1.25, 2.0, -1.0):
+            with pytest.raises(AssertionError, match=name):
+                L.check_slopes([t * factor if i == n else t for i, t in enumerate(good)], do, dl, q, k, v, True, scale)
+    no_delta = L.backward64(do, q, k, v, torch.zeros_like(o), lse, True, scale, dl)[0]
+    no_lse = L.backward64(do, q, k, v, o, lse, True, scale)[0]
+    one_head = L.backward64(do[:, :, ::2], q[:, :, ::2], k, v, o[:, :, ::2], lse[:, ::2], True, scale, dl[:, ::2])[0]
+    for bad in ([no_delta[0], good[1], good[2]], [good[0], no_delta[1], good[2]], [no_lse[0], good[1], good[2]], [good[0], no_lse[1], good[2]],
+                [good[0], one_head[1], good[2]], [good[0], good[1], one_head[2]]):
+        with pytest.raises(AssertionError):
+            L.check_slopes(bad, do, dl, q, k, v, True, scale)
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_norm_rope_reference_against_differences(interleaved):
     g = torch.Generator().manual_seed(6)

@@ -131,6 +131,17 @@ def test_backward_against_differences():
         assert abs((hi - lo) - want) <= 4 * math.sqrt(2) * o_round + 4 * L.H * size + 0.1 * size * math.sqrt(8), (n, hi - lo, want)
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,Sq,Skv,causal", [(1, 4, 2, 150, 150, True), (2, 2, 2, 70, 40, True), (1, 3, 1, 33, 200, False)])
+def test_backward_against_differences_along_its_signs(B, Hq, Hkv, Sq, Skv, causal):
+    """The gradient from the forward pass's own O and LSE; a factor or a lost term does not pass (layer_util.check_slopes)."""
+    do, q, k, v, _, lse, dl = inputs(B, Hq, Hkv, Sq, Skv, causal, seed=2450, dlse=True)
+    dl = 4 * dl.masked_fill(torch.isneginf(lse), 0.0)       # (rows without a key: LSE is -inf, and no slope of it)
+    d = cuda(do, q, k, v, dl)
+    o, lse = A.attention(*d[1:4], causal=causal)
+    grads = A.attention_backward(*d[:4], o, lse, causal=causal, dlse=d[4])
+    L.check_slopes(grads, do, dl, q, k, v, causal, SCALE)
+
+
 def test_backward_refuses():
     do, q, k, v, o, lse, dl = cuda(*inputs(2, 4, 2, 20, 30, True, seed=2500, dlse=True))
     good = dict(do=do, q=q, k=k, v=v, o=o, lse=lse, dlse=dl)
