@@ -39,8 +39,9 @@ extern "C" {
  *   workspace      at least attn_bwd_workspace(...) bytes, 16-byte aligned; contents need not be set and are not kept
  *   B, Hq, Hkv, Sq, Skv, D, causal, scale   as in attn_fwd
  *
- * Masked pairs take no part, whatever they hold, but for one thing: a value that is not finite in a row of q or dout, or of k,
- * makes the gradients of the keys, or queries, that are masked for it but lie within 160 positions of one that is not, NaN.
+ * Masked pairs take no part, whatever they hold, but for one thing: a value that is not finite in row i of q or dout also makes the
+ * gradients of keys NaN that are masked for it, but none from i + Skv - Sq + 160 on; and one in key j of k those of query rows that it is masked for, but none up
+ * to j - (Skv - Sq) - 160.  (Sums run over whole tiles, with a probability of 0 where a pair is masked, and 0 times such a value is NaN.)
  * Size limits (ATTN_E_UNSUPPORTED): D, Sq + Skv, Hq and Hkv as in attn_fwd; B * Hkv * ceil(Skv / 128) and B * Hq / p * ceil(Sq * p / 128), p = 4, 2
  * or 1 the largest that divides Hq / Hkv, below 2^23.  ATTN_E_WORKSPACE if the workspace is too small.
  */

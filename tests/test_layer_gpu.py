@@ -142,6 +142,82 @@ def test_backward_against_differences_along_its_signs(B, Hq, Hkv, Sq, Skv, causa
     L.check_slopes(grads, do, dl, q, k, v, causal, SCALE)
 
 
+NOT_FINITE = [(1, 4, 2, 500, 500), (2, 2, 1, 200, 450), (1, 2, 2, 450, 200), (24, 8, 8, 200, 200)]
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("shape", NOT_FINITE, ids=str)
+def test_backward_of_values_that_are_not_finite(shape, value):
+    """Under the mask: NaN where the formulas have it, the same bits in what such a value is masked for, from 160 positions on (a value of v, o or of
+    LSE's gradient: from the first position on) and in other heads and batch entries.  (An infinity leaves infinities as well: P > 0 times one is one.)"""
+    B, Hq, Hkv, Sq, Skv = shape
+    G, off, nan = Hq // Hkv, Skv - Sq, math.isnan(value)
+    clean = inputs(*shape, True, seed=2800, dlse=True)
+    want = A.attention_backward(*cuda(*clean[:6]), causal=True, dlse=clean[6].cuda())
+    names = ("do", "q", "k", "v", "o", "lse", "dlse")
+    b, h = B - 1, G - 1             # the head of a group's queries, the first of the keys
+
+    def run(**changed):
+        t = {**dict(zip(names, clean)), **changed}
+        got = A.attention_backward(*cuda(*(t[n] for n in names[:6])), causal=True, dlse=t["dlse"].cuda())
+        return [x.cpu() for x in got]
+
+    def same(got, ref, but=slice(None), heads=slice(0, 0)):
+        """Everything the same but positions `but` of heads `heads` of batch entry b, which are returned."""
+        ref, x = ref.cpu(), got.clone()
+        part = got[b, but, heads].float()
+        x[b, but, heads] = ref[b, but, heads]
+        assert torch.equal(x, ref)
+        return part
+
+    bad = lambda name, *at: (lambda t: (t.__setitem__(at, value), t)[1])(clean[names.index(name)].clone())
+    spoilt = lambda x: torch.isnan(x).all() if nan else not torch.isfinite(x).any()
+    group = slice(0, 1)
+    for i in sorted({0, max(0, -off - 1), max(0, -off), 37, Sq // 2, Sq - 1}):
+        seen = max(0, i + off + 1)          # keys that row i sees
+        reach = min(Skv, max(0, i + off + 160))
+        row = (slice(i, i + 1), slice(h, h + 1))
+        for name, column in (("q", 5), ("do", 77)):
+            x = bad(name, b, i, h, column)
+            changed = {name: x}
+            if name == "q":
+                changed["lse"] = clean[5].clone()
+                if seen:
+                    changed["lse"][b, h, i] = math.nan
+            dq, dk, dv = run(**changed)
+            part = same(dq, want[0], *row)
+            assert spoilt(part) if seen else (part == 0).all()
+            part = same(dk, want[1], slice(0, reach), group)
+            assert spoilt(part[:seen])
+            part = same(dv, want[2], slice(0, reach), group)
+            assert spoilt(part[:seen, :, 77]) and (name == "q" or torch.equal(dv[..., :77], want[2].cpu()[..., :77]))
+        for name, at in (("o", (b, i, h, 3)), ("dlse", (b, h, i))):
+            dq, dk, dv = run(**{name: bad(name, *at)})
+            part = same(dq, want[0], *row)
+            assert not torch.isfinite(part).any() if seen else (part == 0).all()
+            part = same(dk, want[1], slice(0, seen), group)
+            assert not torch.isfinite(part).any()
+            same(dv, want[2])
+    for j in sorted({0, 100, Skv // 2, Skv - 33, Skv - 1}):
+        sees = max(0, j - off)              # the first row that sees key j
+        for name in ("k", "v"):
+            changed = {name: bad(name, b, j, 0, 9)}
+            if name == "k":
+                changed["lse"] = clean[5].clone()
+                changed["lse"][b, :G, sees:] = math.nan
+            else:
+                changed["o"] = clean[4].clone()
+                changed["o"][b, sees:, :G, 9] = value
+            dq, dk, dv = run(**changed)
+            part = same(dq, want[0], slice(max(0, sees - 159) if name == "k" else sees, Sq), slice(0, G))
+            assert spoilt(part[-(Sq - sees):])
+            same(dk, want[1], slice(0, Skv), group)
+            if name == "k":
+                same(dv, want[2], slice(0, Skv), group)
+            else:
+                same(dv, want[2])
+
+
 def test_backward_refuses():
     do, q, k, v, o, lse, dl = cuda(*inputs(2, 4, 2, 20, 30, True, seed=2500, dlse=True))
     good = dict(do=do, q=q, k=k, v=v, o=o, lse=lse, dlse=dl)
@@ -321,6 +397,29 @@ def test_norm_rope_backward_of_places_outside_the_table(S, dtype):
         (ref, bound), (ref_w, bound_w) = L.norm_rope_backward64(dz.masked_fill(out[:, :, None, None], 0.0), t, w, cos, sin, at, 1e-6, False)
         L.check_close(x[~out.cuda()], (ref[~out], bound[~out]), f"d{name}")
         L.check_close(dw, (ref_w, bound_w), f"d{name}_weight")
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_norm_rope_of_values_that_are_not_finite(value):
+    """They stay in their own head of their own token, but for the weights' gradients, which are sums over all."""
+    q, k, dq, dk = (L.rand(40 + n, 2, 50, h, 128) for n, h in enumerate((4, 2, 4, 2)))
+    w, cos, sin = torch.ones(128), *L.table(50, 128)
+    forward = lambda q: A.qk_norm_rope(*cuda(q, k, w, w, cos, sin), v=k.cuda())
+    backward = lambda dq, q: A.qk_norm_rope_backward(*cuda(dq, dk, q, k, w, w, cos, sin))
+    bad = lambda t: t.index_put((torch.tensor(1), torch.tensor(17), torch.tensor(2), torch.tensor(60)), torch.tensor(value, dtype=t.dtype))
+    for want, got in ((forward(q), forward(bad(q))), (backward(dq, q), backward(dq, bad(q))), (backward(dq, q), backward(bad(dq), q))):
+        a, x = want[0], got[0].clone()
+        assert not torch.isfinite(x[1, 17, 2]).all()
+        x[1, 17, 2] = a[1, 17, 2]
+        assert torch.equal(x, a) and torch.equal(got[1], want[1])
+        if len(got) == 3:           # values
+            assert torch.equal(got[2], want[2])
+        else:
+            assert not torch.isfinite(got[2]).all() and torch.equal(got[3], want[3])
+    odd = torch.tensor([0x7fc1, 0xffff - 65536, 0x7f80, 0xff80 - 65536, 0x8000 - 65536, 1], dtype=torch.int16).view(torch.bfloat16)
+    v = k.clone()
+    v[1, 3, 1, :6] = odd
+    assert torch.equal(A.qk_norm_rope(*cuda(q, k, w, w, cos, sin), v=v.cuda())[2].cpu().view(torch.int16), v.view(torch.int16))       # bit by bit
 
 
 def test_norm_rope_zeros_and_extremes():
