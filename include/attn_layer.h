@@ -85,7 +85,8 @@ typedef struct {
  *     y = x / sqrt(mean(x^2) + eps) * weight;  each rotated pair (a, b) of y becomes (a cos - b sin, b cos + a sin)
  * with cos and sin of the token's table row; computed in FP32, rounded to BF16 once.  v, where given (v_in->ptr not NULL), is
  * copied, so that slices of one projection come out as the contiguous tensors that attn_fwd takes, in one pass.
- * A token whose place lies outside the table gets NaN in q and k.
+ * A token whose place lies outside the table gets NaN in q and k.  The squares too are FP32: a head whose 2-norm is beyond 1.8e19 comes out as zeros
+ * (and has no gradient), and one whose mean square and eps together are below 1.2e-38 loses precision.
  * Size limits (ATTN_E_UNSUPPORTED), for both directions: B * S * Hq and B * S * Hkv at most 2^31 - 2^16; here also the heads of all tokens,
  * B * S * (Hq + Hkv), or B * S * (Hq + 2 * Hkv) with v, below 2^29 - 96.
  */

@@ -57,6 +57,14 @@ def test_backward_scales(scale, causal):
     L.check_backward(got, L.backward64(do, q, k, v, o, lse, causal, scale), f"scale {scale}")
 
 
+@pytest.mark.parametrize("scale", [1.2e-38, 1e-40, -1e-44, 1e-46])
+def test_backward_of_scales_below_the_normal_range(scale):
+    """Scores of no size beside a mask of infinity: all keys that a row sees have the same probability.  (In FP32 the last of them is 0.)"""
+    do, q, k, v, o, lse, dl = inputs(1, 4, 2, 70, 90, True, seed=2050, scale=scale, dlse=True)
+    got = A.attention_backward(*cuda(do, q, k, v, o, lse), causal=True, scale=scale, dlse=dl.cuda())
+    L.check_backward(got, L.backward64(do, q, k, v, o, lse, True, scale, dl), f"scale {scale}")
+
+
 def test_backward_of_rows_without_a_key():
     """Under the mask, with more queries than keys, the first rows see nothing: no gradient of theirs, whatever arrives."""
     do, q, k, v, o, lse, dl = inputs(1, 2, 1, 170, 100, True, seed=2100, dlse=True)
@@ -397,6 +405,25 @@ def test_norm_rope_backward_of_places_outside_the_table(S, dtype):
         (ref, bound), (ref_w, bound_w) = L.norm_rope_backward64(dz.masked_fill(out[:, :, None, None], 0.0), t, w, cos, sin, at, 1e-6, False)
         L.check_close(x[~out.cuda()], (ref[~out], bound[~out]), f"d{name}")
         L.check_close(dw, (ref_w, bound_w), f"d{name}_weight")
+
+
+def test_norm_rope_beyond_the_squares_range():
+    """Heads whose squares add up to more than FP32 holds come out as zeros, and so do their gradients; their neighbours do not notice."""
+    q, dq = L.rand(50, 1, 6, 2, 128), L.rand(51, 1, 6, 2, 128)
+    q[0, 2, 0, 7], q[0, 4, 1] = 1e20, 3e38
+    cos, sin = L.table(6, 128)
+    at, big = torch.arange(6)[None], torch.zeros(1, 6, 2, dtype=torch.bool)
+    big[0, 2, 0] = big[0, 4, 1] = True
+    w = torch.ones(128)
+    got = A.qk_norm_rope(*cuda(q, q, w, w, cos, sin))[0].cpu()
+    ref, bound = L.norm_rope64(q, w, cos, sin, at, 1e-6, False)
+    assert not got[big].any()
+    L.check_close(got[~big], (ref[~big], bound[~big]))
+    dx, _, dw, _ = A.qk_norm_rope_backward(*cuda(dq, dq, q, q, w, w, cos, sin))
+    (ref, bound), want_w = L.norm_rope_backward64(dq.masked_fill(big[..., None], 0.0), q, w, cos, sin, at, 1e-6, False)
+    assert not dx.cpu()[big].any()
+    L.check_close(dx.cpu()[~big], (ref[~big], bound[~big]))
+    L.check_close(dw, want_w)
 
 
 @pytest.mark.parametrize("value", [math.nan, math.inf])
