@@ -17,10 +17,12 @@
 // With v_mfma_f32_32x32x16_bf16 and Y as the A operand, the accumulator layout puts one held row (lane % 32) in each lane
 // and 16 of the tile's 32 streamed rows in its registers, so P and dS are, packed to BF16 in registers, directly the B operands of the
 // products with Y^T, which the transposing read ds_read_b64_tr_b16 fetches from the same tile in LDS: nothing
-// of size rows x keys leaves the registers.
+// of size rows x keys leaves the registers.  BF16 is what the instruction multiplies, and what the forward pass rounds its P to: with it the 2-norm of the error against
+// 64 bits is 0.0024 of the result's in every call timed, of which the rounding of the results alone is 0.0017; P and dS in two BF16 parts each would be twice the
+// products.
 //
-// What bounds it: 14 * 128 FLOP per pair of unmasked row and key on the matrix pipe.  8 x 4096, 16 heads: 3.15 ms, 1.22 PFLOP/s of products (a library
-// product of 8192^3 on the same card 1.24), the pipe 74 % busy at the 1.56 GHz that the board's power leaves; memory reads and writes are
+// What bounds it: 14 * 128 FLOP per pair of unmasked row and key on the matrix pipe.  8 x 4096, 16 heads: 3.06 ms, 1.26 PFLOP/s of products (a library
+// product of 8192^3 on the same card as much), the pipe 75 % busy at the 1.56 GHz that the board's power leaves; memory reads and writes are
 // 0.4 ms of it.  A wavefront holds 32 rows, a workgroup is four of them, and two workgroups share a compute unit: one's vector
 // instructions, LDS latencies, first loads and results pass behind the other's products.  The step's order and the place of every vector instruction in it
 // are fixed by hand (sched_barrier), because the registers, 256 per wavefront of which sums and held operands take 160, leave no room for the

@@ -180,9 +180,9 @@ inline void deal(Sizes &p)
     p.xcd_groups = groups % 8 == 0 ? groups / 8 : 0;
     // Keys and rows items read the same inputs.  Side by side they find them in L2, which pays where a few tiles to a group leave the rest of the
     // traffic to memory and the cache behind the L2s does not hold the inputs, unless an item is so long that it must not start late: more than a
-    // quarter of a place's work.  Together / apart, inputs from memory, us: 96 x 300, 16 heads, masked 347 / 387; 210 x 198, 8 heads, masked 228 / 252;
-    // 27 x 642, 24 heads 589 / 626; 34 x 840, 32 on 8 heads 1414 / 1555; longer items 4 x 2401, 32 on 4, masked 877 / 753; smaller inputs 512 x 64, 4 heads,
-    // masked 89 / 86.  Of 60 calls drawn 27 are dealt together: 4.4 % faster on average, between 11 % faster and 1.8 % slower.
+    // quarter of a place's work.  Together / apart, inputs from memory, us: 96 x 300, 16 heads, masked 338 / 382; 210 x 198, 8 heads, masked 227 / 257;
+    // 27 x 642, 24 heads 564 / 583; 34 x 840, 32 on 8 heads 1354 / 1432; longer items 4 x 2401, 32 on 4, masked 865 / 727; smaller inputs 512 x 64, 4 heads,
+    // masked 90 / 86.  40 drawn calls that are dealt together: 5.9 % faster on average, 0.5 to 11.5 %.
     p.together = false;
     if (p.xcd_groups && both < PLACES / 8 && 2.0 * ROW_BYTES * ((double)p.G * p.Sq + p.Skv) * groups > CACHE_BYTES) {
         double all = 0;

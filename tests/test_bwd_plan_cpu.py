@@ -104,12 +104,10 @@ def test_sizes_at_the_limits(checked, causal):
         assert rc == (A.ATTN_OK if _within_limits(*c) else A.ATTN_E_UNSUPPORTED), (c, rc)
 
 
-@pytest.mark.parametrize("xcd_groups", [5, 7, 11, 13, 62, 97, 101, 2 * 53, 3 * 37, 131, 997, 131071])
-@pytest.mark.parametrize("S", [64, 300, 1000, 4096])
+@pytest.mark.parametrize("xcd_groups,S", [(g, S) for g in (5, 7, 11, 13, 62, 97, 101, 2 * 53, 3 * 37, 131, 997, 131071) for S in (64, 300, 1000, 4096)
+                                          if g < 1000 or S == 64])       # (more items than a call may have)
 def test_windows_of_group_counts_without_divisors(plan, lib, xcd_groups, S):
     """An XCD's 64 places are not asked to take more than twice their items at a time because its groups divide badly, nor to look for divisors."""
-    if S > 64 and xcd_groups > 1000:
-        pytest.skip("more items than a call may have")
     call = (xcd_groups, 8, 8, S, S, False)
     p = plan(*call)
     assert p["xcd_groups"] == xcd_groups
